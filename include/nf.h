@@ -53,7 +53,7 @@ enum nf_status {
 /* bits of the device status word */
 enum nf_device_flag {
   NF_ELABEL = 1,     /* a label was outside [0, classes); it was clamped */
-  NF_ENONFINITE = 2, /* the loss was NaN or infinite */
+  NF_ENONFINITE = 2, /* the loss was NaN or infinite; nf_cache_quantize: a value was */
   NF_ETIMEOUT = 4,   /* a bounded wait inside a kernel ran out; results of that step are invalid */
   NF_EINDEX = 8      /* nf_cache_gather: an index was outside [0, cache_rows); that output row was zero-filled */
 };
@@ -323,6 +323,62 @@ int nf_conv3x3_wgrad(int dtype, const void* x, const void* g, int N, int H, int 
 #define NF_STATIC_SCRATCH_BYTES (16u << 20)
 int nf_conv3x3_wgrad_static(int dtype, const void* x, const void* g, int N, int H, int W, int Cin, int Cout,
                             int stride, float* dw);
+
+/* Operators for the parts of a step that a caller composes: normalisation that needs no batch, linear layers, dropout, and the
+ * activation cache in 8 bits.  (The paper's networks are VGG and ResNet shapes: a classifier of linear layers with dropout stands
+ * behind their last block, 1x1 convolutions are linear layers over pixels, and at the batch sizes of a few images that small memory
+ * budgets force, group normalisation replaces batch statistics.)  All pointers device unless said otherwise, 16-byte aligned, tensors dense and
+ * channels-last; outputs must not share memory with inputs except where a call says so.  Parameters, statistics and parameter gradients are float,
+ * activations and their gradients of `dtype`, linear weights of `dtype`.  Arithmetic and sums in fp32 or more, each output rounded once.
+ * Results do not depend on launch order: the same call on the same data gives the same bits.  Asynchronous on the library's stream, and
+ * recordable into a CUDA graph after a first eager call with the same arguments.  Concurrent calls need scratch of their own. */
+enum nf_act { NF_ACT_NONE = 0, NF_ACT_RELU = 1, NF_ACT_SILU = 2, NF_ACT_GELU = 3 };  /* GELU: z times the normal distribution function of z */
+
+/* Group normalisation with the activation behind it.  x, y: [N][P][C], P pixels per image; the C channels form `groups` groups of
+ * neighbours; gamma, beta: [C]; mean, rstd: [N][groups] (written, for the backward pass):
+ *   y = act(gamma xh + beta),  xh = (x - mean) rstd,  rstd = 1 / sqrt(variance + eps), biased variance over P * C/groups values.
+ * Backward: dy the gradient at y; dx the gradient at x; dgamma, dbeta: [C].  Needs nf_group_norm_scratch_bytes() of scratch (overwritten).
+ * NF_EINVAL: sizes < 1, C not a multiple of groups, eps not above 0; NF_EUNSUPPORTED: more than 4096 channels in a group. */
+int nf_group_norm_forward(int dtype, const void* x, const float* gamma, const float* beta, int N, int P, int C, int groups, float eps, int act,
+                          void* y, float* mean, float* rstd);
+size_t nf_group_norm_scratch_bytes(int dtype, int N, int P, int C, int groups);
+int nf_group_norm_backward(int dtype, const void* x, const void* dy, const float* gamma, const float* beta, const float* mean, const float* rstd,
+                           int N, int P, int C, int groups, int act, void* scratch, size_t scratch_bytes, void* dx, float* dgamma, float* dbeta);
+
+/* Linear layer over M rows: x [M][K], w [N][K], y = act(x w^T + bias + residual) [M][N].  bias: float [N] or NULL; residual: [M][N] of dtype or
+ * NULL, joins before the activation like the shortcut of nf_layer_set_skip; pre: [M][N] of dtype or NULL, receives the value before the activation
+ * (SiLU and GELU need it in the backward pass; for ReLU y does).  The backward pass is up to three calls, each a tensor the caller keeps:
+ *   nf_act_backward: g = dy act'(saved), n elements; saved = pre, or for ReLU y.  g is the gradient at the sum, so the residual's too; it may
+ *                    be dy's or saved's memory.  Not needed without an activation: then g = dy.
+ *   nf_linear_dgrad: dx = g w [M][K].
+ *   nf_linear_wgrad: dw = g^T x, float [N][K]; db = column sums of g, float [N], or NULL.
+ * All but nf_act_backward need nf_linear_scratch_bytes() of scratch (overwritten).  fp32 operands have to be finite and below 2^127 in
+ * magnitude: an infinity among them may give NaN instead of an infinity. */
+int nf_linear_forward(int dtype, const void* x, const void* w, const float* bias, const void* residual, int M, int K, int N, int act, void* scratch,
+                      size_t scratch_bytes, void* pre, void* y);
+int nf_act_backward(int dtype, int act, const void* saved, const void* dy, long long n, void* g);
+int nf_linear_dgrad(int dtype, const void* g, const void* w, int M, int K, int N, void* scratch, size_t scratch_bytes, void* dx);
+int nf_linear_wgrad(int dtype, const void* x, const void* g, int M, int K, int N, void* scratch, size_t scratch_bytes, float* dw, float* db);
+size_t nf_linear_scratch_bytes(int dtype, int M, int K, int N);
+
+/* Dropout with probability p in [0, 1): y[i] = 0 where u(i) < floor(p 2^32), else x[i] / (1 - p).  u(i) is word i % 4 of
+ * Philox4x32-10 with key `seed` and counter (i / 4, offset), 64 bits each; the effective offset is offset + *offset_dev where
+ * offset_dev (device, 8-byte aligned) is not NULL, so that a recorded step draws anew when the graph advances a counter.  No mask is
+ * stored: the gradient is the same call on dy with the same seed and offsets.  y may be x.  A dropped infinity or NaN becomes 0. */
+int nf_dropout(int dtype, const void* x, long long n, float p, unsigned long long seed, unsigned long long offset,
+               const unsigned long long* offset_dev, void* y);
+
+/* The activation cache in 8 bits (half of bf16's memory and host-to-device traffic; the paper's cache takes 1.5 to 5.3 times the
+ * data set).  x: [rows][row_elems] of dtype.  A row is cut into groups of `group` (32, 64 or 128) neighbouring elements, the last one may be
+ * shorter; codes: [rows][row_elems] bytes; scales: float [rows][ceil(row_elems / group)].  With a = the group's largest magnitude, at least
+ * 2^-100, and top = 127 (NF_Q_INT8: signed bytes) or 448 (NF_Q_E4M3): scale = a / top, code = the nearest to x * (top / a), ties to even, each of these
+ * operations rounded to fp32.  A group with a NaN or an infinity reads back as NaN and raises NF_ENONFINITE in nf_op_status().
+ * nf_cache_gather_quantized is nf_cache_gather from such a cache: out[i] = codes[idx[i]] * scale, rounded once to dtype; an index outside
+ * [0, cache_rows) gives a zero row, label -1 and NF_EINDEX.  codes and scales may lie in pinned host memory. */
+enum nf_cache_format { NF_Q_INT8 = 0, NF_Q_E4M3 = 1 };
+int nf_cache_quantize(int format, int dtype, const void* x, int rows, long long row_elems, int group, void* codes, float* scales);
+int nf_cache_gather_quantized(int format, const void* codes, const float* scales, const int32_t* cache_labels, int cache_rows, const int32_t* idx,
+                              int count, long long row_elems, int group, int dtype, void* out, int32_t* out_labels);
 
 /* Algorithm 1 (host only, no device work): given each layer's largest feasible batch size,
  * cap at B and group consecutive layers while |b[i+1]-b[i]| <= rho*b[i]; a block's batch size

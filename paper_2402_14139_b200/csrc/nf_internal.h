@@ -134,8 +134,31 @@ static inline void nf_launch(void (*kernel)(P...), dim3 grid, dim3 block, size_t
   cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);  // an error stays as the last error, which NF_LAUNCHED reads
 }
 
+// The same for a kernel whose blocks work in clusters of `cluster`
+template <typename... P, typename... A>
+static inline void nf_launch_cluster(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, unsigned cluster, A&&... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = nf_stream();
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = cluster;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = t_nf_route.plain ? 1 : 2;
+  t_nf_route.plain = false;
+  cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
+
 static inline size_t nf_align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 static inline size_t nf_esize(int dtype) { return dtype == NF_F32 ? 4 : 2; }
+static inline bool nf_overlap(const void* a, size_t na, const void* b, size_t nb) {
+  return a && b && (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+}
 
 // ---- generic CUDA-core kernels (nf_direct.cu, nf_elem.cu): any shape, fp32 or bf16 storage, fp32 accumulate
 int nf_k_conv(int dtype, const void* x, int N, int H, int W, int Ci, const void* w, long ws_tap, long ws_co,

@@ -1,0 +1,231 @@
+// Linear layers: y = act(x w^T + bias + residual), and the products its gradients are made of.
+//
+//   forward  y[m][n]  = sum_k x[m][k] w[n][k]      dgrad  dx[m][k] = sum_n g[m][n] w[n][k]      wgrad  dw[n][k] = sum_m g[m][n] x[m][k]
+//
+// All three are C[p][q] = sum_r A(p, r) B(q, r) with operands that are contiguous along r or along p / q.
+#include <initializer_list>
+
+#include "nf_act.cuh"
+#include "nf_ldst.cuh"
+
+namespace {
+
+struct Epilogue {
+  const float* bias;
+  const void* residual;
+  int act;
+  void* pre;
+  void* out;
+  int out_f32;  // out is float whatever the operands' type
+};
+
+// The sum at (p, q) to its place: bias and residual are added in fp32, every stored value is rounded once
+template <typename T>
+__device__ __forceinline__ void finish(const Epilogue& e, size_t at, int q, float v) {
+  if (e.out_f32) {
+    reinterpret_cast<float*>(e.out)[at] = v;
+    return;
+  }
+  if (e.bias) v += e.bias[q];
+  if (e.residual) v += ldf(reinterpret_cast<const T*>(e.residual), at);
+  if (e.pre) stf(reinterpret_cast<T*>(e.pre), at, v);
+  stf(reinterpret_cast<T*>(e.out), at, nf_act_value<T>(v, e.act));
+}
+
+// 64 x 64 results per block, 4 x 4 per thread, 16 steps of r at a time; sa_p, sa_r: element strides of A.  gridDim.z > 1: each z sums a
+// range of r into part[z][P][Q].
+template <typename T>
+__global__ void __launch_bounds__(256) gemm_simple_kernel(const T* __restrict__ A, size_t sa_p, size_t sa_r, const T* __restrict__ B, size_t sb_q,
+                                                          size_t sb_r, int P, int Q, int R, float* part, const Epilogue e) {
+  nf_pdl_begin();
+  __shared__ float As[16][68], Bs[16][68];
+  const int p0 = blockIdx.x * 64, q0 = blockIdx.y * 64;
+  const int r_lo = (int)((long long)R * blockIdx.z / gridDim.z), r_hi = (int)((long long)R * (blockIdx.z + 1) / gridDim.z);
+  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+  float acc[4][4] = {};
+  for (int r0 = r_lo; r0 < r_hi; r0 += 16) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int l = threadIdx.x + 256 * i;
+      // neighbouring threads along whichever direction is contiguous
+      const int pa = sa_r == 1 ? l / 16 : l % 64, ra = sa_r == 1 ? l % 16 : l / 64;
+      As[ra][pa] = p0 + pa < P && r0 + ra < r_hi ? ldf(A, (size_t)(p0 + pa) * sa_p + (size_t)(r0 + ra) * sa_r) : 0.f;
+      const int qb = sb_r == 1 ? l / 16 : l % 64, rb = sb_r == 1 ? l % 16 : l / 64;
+      Bs[rb][qb] = q0 + qb < Q && r0 + rb < r_hi ? ldf(B, (size_t)(q0 + qb) * sb_q + (size_t)(r0 + rb) * sb_r) : 0.f;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      float a[4], b[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a[i] = As[k][ty * 4 + i];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) b[j] = Bs[k][tx * 4 + j];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(a[i], b[j], acc[i][j]);
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int p = p0 + ty * 4 + i, q = q0 + tx * 4 + j;
+      if (p >= P || q >= Q) continue;
+      const size_t at = (size_t)p * Q + q;
+      if (gridDim.z > 1)
+        part[(size_t)blockIdx.z * P * Q + at] = acc[i][j];
+      else
+        finish<T>(e, at, q, acc[i][j]);
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) gemm_join_kernel(const float* __restrict__ part, int splits, size_t n, int Q, const Epilogue e) {
+  nf_pdl_begin();
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  double s = 0;
+  for (int z = 0; z < splits; ++z) s += part[(size_t)z * n + i];
+  finish<T>(e, i, (int)(i % Q), (float)s);
+}
+
+// part[block][n]: sums of g over a range of rows
+template <typename T>
+__global__ void __launch_bounds__(256) column_sums_kernel(const T* __restrict__ g, int M, int N, float* __restrict__ part) {
+  nf_pdl_begin();
+  __shared__ float sm[8][32];
+  const int tx = threadIdx.x % 32, ty = threadIdx.x / 32, n = blockIdx.y * 32 + tx;
+  const int m0 = (int)((long long)M * blockIdx.x / gridDim.x), m1 = (int)((long long)M * (blockIdx.x + 1) / gridDim.x);
+  float s = 0;
+  if (n < N)
+    for (int m = m0 + ty; m < m1; m += 8) s += ldf(g, (size_t)m * N + n);
+  sm[ty][tx] = s;
+  __syncthreads();
+  if (ty == 0 && n < N) {
+#pragma unroll
+    for (int k = 1; k < 8; ++k) s += sm[k][tx];
+    part[(size_t)blockIdx.x * N + n] = s;
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) act_backward_kernel(const T* saved, const T* dy, size_t n, int act, T* g) {
+  nf_pdl_begin();
+  const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 8;
+  if (i >= n) return;
+  if (i + 8 <= n) {
+    float s[8], d[8];
+    ld8(saved + i, s);
+    ld8(dy + i, d);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) d[e] *= nf_act_grad<T>(s[e], act);
+    st8(g + i, d);
+  } else {
+    for (size_t e = i; e < n; ++e) stf(g, e, ldf(dy, e) * nf_act_grad<T>(ldf(saved, e), act));
+  }
+}
+
+int simple_splits(int P, int Q, int R) {
+  const long tiles = (long)((P + 63) / 64) * ((Q + 63) / 64);
+  long s = 296 / tiles;
+  if (s > R / 256) s = R / 256;
+  return s < 1 ? 1 : (int)s;
+}
+
+template <typename T>
+int gemm(const void* A, size_t sa_p, size_t sa_r, const void* B, size_t sb_q, size_t sb_r, int P, int Q, int R, float* part, const Epilogue& e) {
+  const int splits = simple_splits(P, Q, R);
+  if ((P + 63) / 64 > 0x7fffffff || (Q + 63) / 64 > 65535) return NF_EUNSUPPORTED;
+  nf_launch(gemm_simple_kernel<T>, dim3((P + 63) / 64, (Q + 63) / 64, splits), 256, 0, (const T*)A, sa_p, sa_r, (const T*)B, sb_q, sb_r, P, Q, R,
+            part, e);
+  NF_LAUNCHED();
+  if (splits > 1) {
+    const size_t n = (size_t)P * Q;
+    nf_launch(gemm_join_kernel<T>, (unsigned)((n + 255) / 256), 256, 0, (const float*)part, splits, n, Q, e);
+    NF_LAUNCHED();
+  }
+  return NF_OK;
+}
+
+int sum_blocks(int M) { return M < 148 * 8 ? (M + 7) / 8 : 148; }
+
+size_t split_bytes(int P, int Q, int R) {
+  const int s = simple_splits(P, Q, R);
+  return s > 1 ? (size_t)s * P * Q * 4 : 0;
+}
+
+bool sizes_ok(int dtype, int M, int K, int N) { return (dtype == NF_F32 || dtype == NF_BF16) && M >= 1 && K >= 1 && N >= 1; }
+
+}  // namespace
+
+extern "C" size_t nf_linear_scratch_bytes(int dtype, int M, int K, int N) {
+  if (!sizes_ok(dtype, M, K, N)) return 0;
+  size_t b = split_bytes(M, N, K), c = split_bytes(M, K, N), d = split_bytes(N, K, M);
+  if (c > b) b = c;
+  if (d > b) b = d;
+  return b + (size_t)sum_blocks(M) * N * 4 + 256;
+}
+
+extern "C" int nf_linear_forward(int dtype, const void* x, const void* w, const float* bias, const void* residual, int M, int K, int N, int act,
+                                 void* scratch, size_t scratch_bytes, void* pre, void* y) {
+  if (!x || !w || !scratch || !y || !sizes_ok(dtype, M, K, N) || !nf_act_ok(act)) return NF_EINVAL;
+  if (((uintptr_t)x | (uintptr_t)w | (uintptr_t)bias | (uintptr_t)residual | (uintptr_t)scratch | (uintptr_t)pre | (uintptr_t)y) & 15) return NF_EALIGN;
+  const size_t es = nf_esize(dtype), xb = es * M * K, wb = es * N * K, yb = es * M * N;
+  for (const void* o : {(const void*)y, (const void*)pre})
+    if (nf_overlap(o, yb, x, xb) || nf_overlap(o, yb, w, wb) || nf_overlap(o, yb, residual, yb) || nf_overlap(o, yb, bias, (size_t)N * 4))
+      return NF_EINVAL;
+  if (nf_overlap(y, yb, pre, yb)) return NF_EINVAL;
+  if (scratch_bytes < nf_linear_scratch_bytes(dtype, M, K, N)) return NF_ENOWS;
+  const Epilogue e{bias, residual, act, pre, y, 0};
+  return dtype == NF_F32 ? gemm<float>(x, K, 1, w, K, 1, M, N, K, (float*)scratch, e) : gemm<bf16>(x, K, 1, w, K, 1, M, N, K, (float*)scratch, e);
+}
+
+extern "C" int nf_linear_dgrad(int dtype, const void* g, const void* w, int M, int K, int N, void* scratch, size_t scratch_bytes, void* dx) {
+  if (!g || !w || !scratch || !dx || !sizes_ok(dtype, M, K, N)) return NF_EINVAL;
+  if (((uintptr_t)g | (uintptr_t)w | (uintptr_t)scratch | (uintptr_t)dx) & 15) return NF_EALIGN;
+  const size_t es = nf_esize(dtype), xb = es * M * K;
+  if (nf_overlap(dx, xb, g, es * M * N) || nf_overlap(dx, xb, w, es * N * K)) return NF_EINVAL;
+  if (scratch_bytes < nf_linear_scratch_bytes(dtype, M, K, N)) return NF_ENOWS;
+  const Epilogue e{nullptr, nullptr, NF_ACT_NONE, nullptr, dx, 0};
+  return dtype == NF_F32 ? gemm<float>(g, N, 1, w, 1, K, M, K, N, (float*)scratch, e) : gemm<bf16>(g, N, 1, w, 1, K, M, K, N, (float*)scratch, e);
+}
+
+extern "C" int nf_linear_wgrad(int dtype, const void* x, const void* g, int M, int K, int N, void* scratch, size_t scratch_bytes, float* dw,
+                               float* db) {
+  if (!x || !g || !scratch || !dw || !sizes_ok(dtype, M, K, N)) return NF_EINVAL;
+  if (((uintptr_t)x | (uintptr_t)g | (uintptr_t)scratch | (uintptr_t)dw | (uintptr_t)db) & 15) return NF_EALIGN;
+  const size_t es = nf_esize(dtype), wb = (size_t)4 * N * K, bb = (size_t)4 * N;
+  if (nf_overlap(dw, wb, x, es * M * K) || nf_overlap(dw, wb, g, es * M * N) || nf_overlap(db, bb, x, es * M * K) ||
+      nf_overlap(db, bb, g, es * M * N) || nf_overlap(dw, wb, db, bb))
+    return NF_EINVAL;
+  if (scratch_bytes < nf_linear_scratch_bytes(dtype, M, K, N)) return NF_ENOWS;
+  const Epilogue e{nullptr, nullptr, NF_ACT_NONE, nullptr, dw, 1};
+  const int rc = dtype == NF_F32 ? gemm<float>(g, 1, N, x, 1, K, N, K, M, (float*)scratch, e) : gemm<bf16>(g, 1, N, x, 1, K, N, K, M, (float*)scratch, e);
+  if (rc != NF_OK || !db) return rc;
+  float* part = (float*)scratch;  // the product's partial sums have been read by now
+  const dim3 grid(sum_blocks(M), (N + 31) / 32);
+  if (dtype == NF_F32)
+    nf_launch(column_sums_kernel<float>, grid, 256, 0, (const float*)g, M, N, part);
+  else
+    nf_launch(column_sums_kernel<bf16>, grid, 256, 0, (const bf16*)g, M, N, part);
+  NF_LAUNCHED();
+  return nf_k_sum_parts(part, sum_blocks(M), N, db, true);
+}
+
+extern "C" int nf_act_backward(int dtype, int act, const void* saved, const void* dy, long long n, void* g) {
+  if (!saved || !dy || !g || n < 1 || (dtype != NF_F32 && dtype != NF_BF16) || !nf_act_ok(act)) return NF_EINVAL;
+  if (((uintptr_t)saved | (uintptr_t)dy | (uintptr_t)g) & 15) return NF_EALIGN;
+  const size_t bytes = (size_t)n * nf_esize(dtype);
+  if ((g != dy && nf_overlap(g, bytes, dy, bytes)) || (g != saved && nf_overlap(g, bytes, saved, bytes))) return NF_EINVAL;
+  const size_t blocks = ((size_t)n + 2047) / 2048;
+  if (blocks > 0x7fffffffull) return NF_EUNSUPPORTED;
+  if (dtype == NF_F32)
+    nf_launch(act_backward_kernel<float>, (unsigned)blocks, 256, 0, (const float*)saved, (const float*)dy, (size_t)n, act, (float*)g);
+  else
+    nf_launch(act_backward_kernel<bf16>, (unsigned)blocks, 256, 0, (const bf16*)saved, (const bf16*)dy, (size_t)n, act, (bf16*)g);
+  NF_LAUNCHED();
+  return NF_OK;
+}

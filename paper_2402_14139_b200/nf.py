@@ -19,6 +19,10 @@ NF_ELABEL, NF_ENONFINITE, NF_ETIMEOUT, NF_EINDEX = 1, 2, 4, 8
 NF_F32, NF_BF16 = 0, 1
 NF_LOSS_CE, NF_LOSS_MSE = 0, 1
 NF_POOL_AVG, NF_POOL_MAX = 0, 1
+NF_ACT_NONE, NF_ACT_RELU, NF_ACT_SILU, NF_ACT_GELU = range(4)
+NF_Q_INT8, NF_Q_E4M3 = 0, 1
+ACTS = dict(none=NF_ACT_NONE, relu=NF_ACT_RELU, silu=NF_ACT_SILU, gelu=NF_ACT_GELU)
+CACHE_FORMATS = dict(int8=NF_Q_INT8, e4m3=NF_Q_E4M3)
 NF_P_W, NF_P_GAMMA, NF_P_BETA, NF_P_WA, NF_P_BA, NF_P_WF, NF_P_BF, NF_P_RMEAN, NF_P_RVAR = range(9)
 NF_K_VALUE, NF_K_MOMENTUM, NF_K_GRAD = 0, 0x100, 0x200
 PARAM_IDS = dict(W=NF_P_W, gamma=NF_P_GAMMA, beta=NF_P_BETA, Wa=NF_P_WA, ba=NF_P_BA, Wf=NF_P_WF, bf=NF_P_BF,
@@ -31,7 +35,9 @@ EXPORTS = ["nf_layer_create", "nf_layer_destroy", "nf_layer_configure", "nf_laye
            "nf_proj_workspace_bytes", "nf_proj_bind_workspace", "nf_proj_set_param", "nf_proj_get_param", "nf_proj_forward",
            "nf_proj_forward_eval", "nf_proj_backward", "nf_layer_stored_tensor", "nf_block_step", "nf_block_step_host", "nf_block_step_host_next", "nf_trace_enable", "nf_trace_read",
            "nf_cache_gather", "nf_selftest_bounded_wait", "nf_conv3x3_forward", "nf_conv3x3_wgrad_scratch_bytes", "nf_conv3x3_wgrad", "nf_conv3x3_wgrad_static", "nf_op_status", "nf_partition", "nf_set_stream", "nf_launch_count",
-           "nf_layer_kernel_family", "nf_strerror", "nf_last_cuda_error"]
+           "nf_layer_kernel_family", "nf_strerror", "nf_last_cuda_error", "nf_group_norm_forward", "nf_group_norm_scratch_bytes",
+           "nf_group_norm_backward", "nf_linear_forward", "nf_act_backward", "nf_linear_dgrad", "nf_linear_wgrad", "nf_linear_scratch_bytes",
+           "nf_dropout", "nf_cache_quantize", "nf_cache_gather_quantized"]
 
 
 class NfError(RuntimeError):
@@ -115,6 +121,20 @@ def lib():
         L.nf_conv3x3_wgrad.argtypes = [C.c_int, vp, vp] + [C.c_int] * 6 + [vp, C.c_size_t, vp]
         L.nf_conv3x3_wgrad_static.argtypes = [C.c_int, vp, vp] + [C.c_int] * 6 + [vp]
         L.nf_selftest_bounded_wait.argtypes = [C.c_ulonglong, vp]
+        i, ll, ull, sz = C.c_int, C.c_longlong, C.c_ulonglong, C.c_size_t
+        L.nf_group_norm_forward.argtypes = [i, vp, fp, fp, i, i, i, i, C.c_float, i, vp, fp, fp]
+        L.nf_group_norm_scratch_bytes.restype = sz
+        L.nf_group_norm_scratch_bytes.argtypes = [i] * 5
+        L.nf_group_norm_backward.argtypes = [i, vp, vp, fp, fp, fp, fp, i, i, i, i, i, vp, sz, vp, fp, fp]
+        L.nf_linear_forward.argtypes = [i, vp, vp, fp, vp, i, i, i, i, vp, sz, vp, vp]
+        L.nf_act_backward.argtypes = [i, i, vp, vp, ll, vp]
+        L.nf_linear_dgrad.argtypes = [i, vp, vp, i, i, i, vp, sz, vp]
+        L.nf_linear_wgrad.argtypes = [i, vp, vp, i, i, i, vp, sz, fp, fp]
+        L.nf_linear_scratch_bytes.restype = sz
+        L.nf_linear_scratch_bytes.argtypes = [i] * 4
+        L.nf_dropout.argtypes = [i, vp, ll, C.c_float, ull, ull, vp, vp]
+        L.nf_cache_quantize.argtypes = [i, i, vp, i, ll, i, vp, fp]
+        L.nf_cache_gather_quantized.argtypes = [i, vp, fp, ip, i, ip, i, ll, i, i, vp, ip]
         L.nf_partition.argtypes = [C.POINTER(C.c_int), C.c_int, C.c_int, C.c_double, C.POINTER(C.c_int),
                                    C.POINTER(C.c_int)]
         L.nf_set_stream.argtypes = [vp]
@@ -539,6 +559,144 @@ def nf_conv3x3_wgrad_static(dtype, x, g, stride, dw):
     N, H, W, Cin = x.shape
     _check(lib().nf_conv3x3_wgrad_static(dtype, _ptr(x), _ptr(g), N, H, W, Cin, g.shape[3], stride, _ptr(dw)),
            "nf_conv3x3_wgrad_static")
+
+
+def _storage(dtype):
+    import torch
+    if dtype not in (NF_F32, NF_BF16):
+        raise NfError(f"dtype: NF_F32 or NF_BF16, not {dtype!r}")
+    return torch.float32 if dtype == NF_F32 else torch.bfloat16
+
+
+def _tensor(what, t, dtype, shape, host_ok=False):
+    """Address of a dense tensor of this type and shape on the current device (host_ok: or in pinned host memory)."""
+    import torch
+    if t.dtype is not dtype or t.shape != shape:
+        raise NfError(f"{what}: want {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise NfError(f"{what}: not dense")
+    if not (t.is_cuda and t.get_device() == torch.cuda.current_device()) and not (host_ok and t.is_pinned()):
+        raise NfError(f"{what}: not on the current CUDA device")
+    return t.data_ptr()
+
+
+def _choice(what, table, key):
+    if key not in table:
+        raise NfError(f"{what}: one of {sorted(table)}, not {key!r}")
+    return table[key]
+
+
+def _param(what, t, shape):
+    import torch
+    return _tensor(what, t, torch.float32, shape)
+
+
+def _scratch(what, t):
+    import torch
+    return _tensor(what, t, torch.uint8, t.shape), t.numel()
+
+
+def nf_group_norm_forward(dtype, x, gamma, beta, groups, eps, act, y, mean, rstd):
+    """y = act(group_norm(x)): x, y [N, ..., C] of dtype (all dimensions between are pixels), gamma, beta float32 [C], act a key of
+    ACTS; mean, rstd float32 [N, groups] are written for the backward pass."""
+    td = _storage(dtype)
+    N, C_ = x.shape[0], x.shape[-1]
+    P = x.numel() // max(1, N * C_)
+    _check(lib().nf_group_norm_forward(dtype, _tensor("x", x, td, x.shape), _param("gamma", gamma, (C_,)), _param("beta", beta, (C_,)), N, P, C_,
+                                       int(groups), float(eps), _choice("act", ACTS, act), _tensor("y", y, td, x.shape),
+                                       _param("mean", mean, (N, groups)), _param("rstd", rstd, (N, groups))), "nf_group_norm_forward")
+
+
+def nf_group_norm_scratch_bytes(dtype, N, P, C_, groups) -> int:
+    return int(lib().nf_group_norm_scratch_bytes(dtype, N, P, C_, groups))
+
+
+def nf_group_norm_backward(dtype, x, dy, gamma, beta, mean, rstd, act, scratch, dx, dgamma, dbeta):
+    """dx, dgamma, dbeta from x, dy and what the forward pass left in mean and rstd [N, groups]; scratch: uint8 tensor of at least
+    nf_group_norm_scratch_bytes(dtype, N, P, C, groups)."""
+    td = _storage(dtype)
+    N, C_ = x.shape[0], x.shape[-1]
+    P, groups = x.numel() // max(1, N * C_), mean.shape[-1]
+    _check(lib().nf_group_norm_backward(dtype, _tensor("x", x, td, x.shape), _tensor("dy", dy, td, x.shape), _param("gamma", gamma, (C_,)),
+                                        _param("beta", beta, (C_,)), _param("mean", mean, (N, groups)), _param("rstd", rstd, (N, groups)), N, P, C_,
+                                        groups, _choice("act", ACTS, act), *_scratch("scratch", scratch), _tensor("dx", dx, td, x.shape),
+                                        _param("dgamma", dgamma, (C_,)), _param("dbeta", dbeta, (C_,))), "nf_group_norm_backward")
+
+
+def nf_linear_scratch_bytes(dtype, M, K, N) -> int:
+    return int(lib().nf_linear_scratch_bytes(dtype, M, K, N))
+
+
+def nf_linear_forward(dtype, x, w, bias, residual, act, scratch, pre, y):
+    """y = act(x w^T + bias + residual): x [M, K], w [N, K], residual, pre, y [M, N] of dtype, bias float32 [N]; bias, residual and pre
+    (the value before the activation, for the backward pass of SiLU and GELU) may be None; scratch: uint8 tensor of at least
+    nf_linear_scratch_bytes(dtype, M, K, N)."""
+    td = _storage(dtype)
+    (M, K), N = x.shape, w.shape[0]
+    _check(lib().nf_linear_forward(dtype, _tensor("x", x, td, (M, K)), _tensor("w", w, td, (N, K)),
+                                   None if bias is None else _param("bias", bias, (N,)),
+                                   None if residual is None else _tensor("residual", residual, td, (M, N)), M, K, N, _choice("act", ACTS, act),
+                                   *_scratch("scratch", scratch), None if pre is None else _tensor("pre", pre, td, (M, N)),
+                                   _tensor("y", y, td, (M, N))), "nf_linear_forward")
+
+
+def nf_act_backward(dtype, act, saved, dy, g):
+    """g = dy * act'(saved), elementwise; saved: the pre-activation, or for ReLU the output.  g may be dy or saved."""
+    td = _storage(dtype)
+    _check(lib().nf_act_backward(dtype, _choice("act", ACTS, act), _tensor("saved", saved, td, dy.shape), _tensor("dy", dy, td, dy.shape), dy.numel(),
+                                 _tensor("g", g, td, dy.shape)), "nf_act_backward")
+
+
+def nf_linear_dgrad(dtype, g, w, scratch, dx):
+    """dx = g w: g [M, N], w [N, K], dx [M, K] of dtype."""
+    td = _storage(dtype)
+    M, (N, K) = g.shape[0], w.shape
+    _check(lib().nf_linear_dgrad(dtype, _tensor("g", g, td, (M, N)), _tensor("w", w, td, (N, K)), M, K, N, *_scratch("scratch", scratch),
+                                 _tensor("dx", dx, td, (M, K))), "nf_linear_dgrad")
+
+
+def nf_linear_wgrad(dtype, x, g, scratch, dw, db=None):
+    """dw = g^T x (float32 [N, K]) and, if db is given, the column sums of g (float32 [N]): x [M, K], g [M, N] of dtype."""
+    td = _storage(dtype)
+    (M, K), N = x.shape, g.shape[1]
+    _check(lib().nf_linear_wgrad(dtype, _tensor("x", x, td, (M, K)), _tensor("g", g, td, (M, N)), M, K, N, *_scratch("scratch", scratch),
+                                 _param("dw", dw, (N, K)), None if db is None else _param("db", db, (N,))), "nf_linear_wgrad")
+
+
+def nf_dropout(dtype, x, p, seed, offset, y, offset_dev=None):
+    """y = x / (1 - p) where the generator keeps an element, else 0; the gradient is the same call on dy.  seed, offset: 64-bit integers;
+    offset_dev: int64 tensor of one element on the device that is added to offset (advance it inside a recorded step).  y may be x."""
+    import torch
+    td = _storage(dtype)
+    m64 = (1 << 64) - 1
+    _check(lib().nf_dropout(dtype, _tensor("x", x, td, x.shape), x.numel(), float(p), int(seed) & m64, int(offset) & m64,
+                            None if offset_dev is None else _tensor("offset_dev", offset_dev, torch.int64, (1,)), _tensor("y", y, td, x.shape)),
+           "nf_dropout")
+
+
+def nf_cache_quantize(fmt, dtype, x, group, codes, scales):
+    """Rows of x [rows, ...] of dtype into the 8-bit cache: codes uint8 of x's shape, scales float32 [rows, ceil(row elements / group)];
+    fmt a key of CACHE_FORMATS, group 32, 64 or 128."""
+    import torch
+    rows = x.shape[0]
+    E = x.numel() // max(1, rows)
+    _check(lib().nf_cache_quantize(_choice("format", CACHE_FORMATS, fmt), dtype, _tensor("x", x, _storage(dtype), x.shape), rows, E, int(group),
+                                   _tensor("codes", codes, torch.uint8, x.shape), _param("scales", scales, (rows, -(-E // int(group))))),
+           "nf_cache_quantize")
+
+
+def nf_cache_gather_quantized(fmt, codes, scales, cache_labels, idx, group, dtype, out, out_labels):
+    """out[i] = row idx[i] of the 8-bit cache, as dtype, and labels likewise (both label tensors or neither).  codes [rows, ...], scales and
+    cache_labels may lie in pinned host memory; idx int32.  Indices outside the cache as in nf_cache_gather."""
+    import torch
+    rows, count = codes.shape[0], idx.numel()
+    E = codes.numel() // max(1, rows)
+    _check(lib().nf_cache_gather_quantized(
+        _choice("format", CACHE_FORMATS, fmt), _tensor("codes", codes, torch.uint8, codes.shape, True),
+        _tensor("scales", scales, torch.float32, (rows, -(-E // int(group))), True),
+        None if cache_labels is None else _tensor("cache_labels", cache_labels, torch.int32, (rows,), True), rows,
+        _tensor("idx", idx, torch.int32, (count,)), count, E, int(group), dtype, _tensor("out", out, _storage(dtype), (count,) + tuple(codes.shape[1:])),
+        None if out_labels is None else _tensor("out_labels", out_labels, torch.int32, (count,))), "nf_cache_gather_quantized")
 
 
 def nf_selftest_bounded_wait(limit_ns: int, waited_ns_out):
