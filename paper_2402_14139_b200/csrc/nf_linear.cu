@@ -6,18 +6,10 @@
 #include <initializer_list>
 
 #include "nf_act.cuh"
+#include "nf_gemm.h"
 #include "nf_ldst.cuh"
 
 namespace {
-
-struct Epilogue {
-  const float* bias;
-  const void* residual;
-  int act;
-  void* pre;
-  void* out;
-  int out_f32;  // out is float whatever the operands' type
-};
 
 // The sum at (p, q) to its place: bias and residual are added in fp32, every stored value is rounded once
 template <typename T>
@@ -128,6 +120,57 @@ __global__ void __launch_bounds__(256) act_backward_kernel(const T* saved, const
   }
 }
 
+// Operand copies for the tensor cores: rows padded to 16 bytes, and fp32 cut into three bf16 parts whose sum is exact (each is the
+// nearest bf16 to what the earlier ones leave).
+template <typename T>
+__global__ void __launch_bounds__(256) parts_kernel(const T* __restrict__ src, size_t rows, int len, int ld, size_t plane, bf16* __restrict__ dst) {
+  nf_pdl_begin();
+  constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  const int per = ld / 8;
+  const size_t r = i / per;
+  const int c = (int)(i - r * per) * 8;
+  if (r >= rows) return;
+  const T* from = src + r * len + c;
+  float v[8];
+  if (c + 8 <= len && len % (16 / (int)sizeof(T)) == 0) {
+    ld8(from, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = c + e < len ? ldf(from, e) : 0.f;
+  }
+#pragma unroll
+  for (int k = 0; k < kParts; ++k) {
+    float h[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[e] = v[e];
+    st8(dst + k * plane + r * ld + c, h);  // h: as stored
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] -= h[e];
+  }
+}
+
+int pad8(int n) { return (n + 7) / 8 * 8; }
+
+// One of the three products as the kernels see it: A [a_rows][a_len] and B [b_rows][b_len] as they lie
+struct Product {
+  int P, Q, R;
+  bool a_along_r, b_along_r;
+  int a_rows() const { return a_along_r ? P : R; }
+  int a_len() const { return a_along_r ? R : P; }
+  int b_rows() const { return b_along_r ? Q : R; }
+  int b_len() const { return b_along_r ? R : Q; }
+};
+
+bool on_tensor_cores(int dtype, const Product& d) {
+  const double work = (double)d.P * d.Q * d.R;
+  return work >= (dtype == NF_BF16 ? 2097152.0 : 134217728.0);
+}
+bool needs_copy(int dtype, int len) { return dtype == NF_F32 || len % 8; }
+size_t copy_bytes(int dtype, int rows, int len) {
+  return needs_copy(dtype, len) ? nf_align_up((size_t)rows * pad8(len) * 2 * (dtype == NF_F32 ? 3 : 1), 256) : 0;
+}
+
 int simple_splits(int P, int Q, int R) {
   const long tiles = (long)((P + 63) / 64) * ((Q + 63) / 64);
   long s = 296 / tiles;
@@ -135,37 +178,81 @@ int simple_splits(int P, int Q, int R) {
   return s < 1 ? 1 : (int)s;
 }
 
+size_t product_bytes(int dtype, const Product& d) {
+  const bool tc = on_tensor_cores(dtype, d);
+  const int s = tc ? nf_gemm_splits(d.P, d.Q, d.R, dtype == NF_F32 ? 3 : 1) : simple_splits(d.P, d.Q, d.R);
+  size_t b = s > 1 ? (size_t)s * d.P * d.Q * 4 : 0;
+  if (tc) b += copy_bytes(dtype, d.a_rows(), d.a_len()) + copy_bytes(dtype, d.b_rows(), d.b_len());
+  return b;
+}
+
 template <typename T>
-int gemm(const void* A, size_t sa_p, size_t sa_r, const void* B, size_t sb_q, size_t sb_r, int P, int Q, int R, float* part, const Epilogue& e) {
-  const int splits = simple_splits(P, Q, R);
-  if ((P + 63) / 64 > 0x7fffffff || (Q + 63) / 64 > 65535) return NF_EUNSUPPORTED;
-  nf_launch(gemm_simple_kernel<T>, dim3((P + 63) / 64, (Q + 63) / 64, splits), 256, 0, (const T*)A, sa_p, sa_r, (const T*)B, sb_q, sb_r, P, Q, R,
-            part, e);
+int join(const float* part, int splits, int P, int Q, const Epilogue& e) {
+  const size_t n = (size_t)P * Q;
+  nf_launch(gemm_join_kernel<T>, (unsigned)((n + 255) / 256), 256, 0, part, splits, n, Q, e);
   NF_LAUNCHED();
-  if (splits > 1) {
-    const size_t n = (size_t)P * Q;
-    nf_launch(gemm_join_kernel<T>, (unsigned)((n + 255) / 256), 256, 0, (const float*)part, splits, n, Q, e);
-    NF_LAUNCHED();
-  }
   return NF_OK;
+}
+
+template <typename T>
+int simple_product(const Product& d, const void* A, const void* B, float* part, const Epilogue& e) {
+  const int splits = simple_splits(d.P, d.Q, d.R);
+  const size_t la = d.a_len(), lb = d.b_len();
+  nf_launch(gemm_simple_kernel<T>, dim3((d.P + 63) / 64, (d.Q + 63) / 64, splits), 256, 0, (const T*)A, d.a_along_r ? la : 1, d.a_along_r ? 1 : la,
+            (const T*)B, d.b_along_r ? lb : 1, d.b_along_r ? 1 : lb, d.P, d.Q, d.R, part, e);
+  NF_LAUNCHED();
+  return splits > 1 ? join<T>(part, splits, d.P, d.Q, e) : NF_OK;
+}
+
+template <typename T>
+int operand(const void* src, int rows, int len, bool along_r, char*& scratch, GemmOperand* o) {
+  const int dtype = sizeof(T) == 4 ? NF_F32 : NF_BF16;
+  *o = {(const bf16*)src, (size_t)len, 0, along_r};
+  if (!needs_copy(dtype, len)) return NF_OK;
+  const int ld = pad8(len);
+  const size_t plane = (size_t)rows * ld, blocks = (plane / 8 + 255) / 256;
+  if (blocks > 0x7fffffffull) return NF_EUNSUPPORTED;
+  nf_launch(parts_kernel<T>, (unsigned)blocks, 256, 0, (const T*)src, (size_t)rows, len, ld, plane, (bf16*)scratch);
+  NF_LAUNCHED();
+  *o = {(const bf16*)scratch, (size_t)ld, plane, along_r};
+  scratch += copy_bytes(dtype, rows, len);
+  return NF_OK;
+}
+
+template <typename T>
+int product(const Product& d, const void* A, const void* B, void* scratch, const Epilogue& e) {
+  const int dtype = sizeof(T) == 4 ? NF_F32 : NF_BF16;
+  if ((d.Q + 63) / 64 > 65535) return NF_EUNSUPPORTED;
+  if (!on_tensor_cores(dtype, d)) return simple_product<T>(d, A, B, (float*)scratch, e);
+  char* s = (char*)scratch;
+  GemmProblem g{};
+  g.P = d.P; g.Q = d.Q; g.R = d.R;
+  g.planes = dtype == NF_F32 ? 3 : 1;
+  g.out_f32 = dtype == NF_F32 || e.out_f32;
+  int rc = operand<T>(A, d.a_rows(), d.a_len(), d.a_along_r, s, &g.A);
+  if (rc == NF_OK) rc = operand<T>(B, d.b_rows(), d.b_len(), d.b_along_r, s, &g.B);
+  if (rc == NF_OK) rc = nf_gemm_tc(g, e, (float*)s);
+  const int splits = nf_gemm_splits(d.P, d.Q, d.R, g.planes);
+  return rc == NF_OK && splits > 1 ? join<T>((const float*)s, splits, d.P, d.Q, e) : rc;
 }
 
 int sum_blocks(int M) { return M < 148 * 8 ? (M + 7) / 8 : 148; }
 
-size_t split_bytes(int P, int Q, int R) {
-  const int s = simple_splits(P, Q, R);
-  return s > 1 ? (size_t)s * P * Q * 4 : 0;
-}
-
 bool sizes_ok(int dtype, int M, int K, int N) { return (dtype == NF_F32 || dtype == NF_BF16) && M >= 1 && K >= 1 && N >= 1; }
+
+Product forward_of(int M, int K, int N) { return {M, N, K, true, true}; }
+Product dgrad_of(int M, int K, int N) { return {M, K, N, true, false}; }
+Product wgrad_of(int M, int K, int N) { return {N, K, M, false, false}; }
 
 }  // namespace
 
 extern "C" size_t nf_linear_scratch_bytes(int dtype, int M, int K, int N) {
   if (!sizes_ok(dtype, M, K, N)) return 0;
-  size_t b = split_bytes(M, N, K), c = split_bytes(M, K, N), d = split_bytes(N, K, M);
-  if (c > b) b = c;
-  if (d > b) b = d;
+  size_t b = 0;
+  for (const Product& d : {forward_of(M, K, N), dgrad_of(M, K, N), wgrad_of(M, K, N)}) {
+    const size_t n = product_bytes(dtype, d);
+    if (n > b) b = n;
+  }
   return b + (size_t)sum_blocks(M) * N * 4 + 256;
 }
 
@@ -180,7 +267,8 @@ extern "C" int nf_linear_forward(int dtype, const void* x, const void* w, const 
   if (nf_overlap(y, yb, pre, yb)) return NF_EINVAL;
   if (scratch_bytes < nf_linear_scratch_bytes(dtype, M, K, N)) return NF_ENOWS;
   const Epilogue e{bias, residual, act, pre, y, 0};
-  return dtype == NF_F32 ? gemm<float>(x, K, 1, w, K, 1, M, N, K, (float*)scratch, e) : gemm<bf16>(x, K, 1, w, K, 1, M, N, K, (float*)scratch, e);
+  const Product d = forward_of(M, K, N);
+  return dtype == NF_F32 ? product<float>(d, x, w, scratch, e) : product<bf16>(d, x, w, scratch, e);
 }
 
 extern "C" int nf_linear_dgrad(int dtype, const void* g, const void* w, int M, int K, int N, void* scratch, size_t scratch_bytes, void* dx) {
@@ -190,7 +278,8 @@ extern "C" int nf_linear_dgrad(int dtype, const void* g, const void* w, int M, i
   if (nf_overlap(dx, xb, g, es * M * N) || nf_overlap(dx, xb, w, es * N * K)) return NF_EINVAL;
   if (scratch_bytes < nf_linear_scratch_bytes(dtype, M, K, N)) return NF_ENOWS;
   const Epilogue e{nullptr, nullptr, NF_ACT_NONE, nullptr, dx, 0};
-  return dtype == NF_F32 ? gemm<float>(g, N, 1, w, 1, K, M, K, N, (float*)scratch, e) : gemm<bf16>(g, N, 1, w, 1, K, M, K, N, (float*)scratch, e);
+  const Product d = dgrad_of(M, K, N);
+  return dtype == NF_F32 ? product<float>(d, g, w, scratch, e) : product<bf16>(d, g, w, scratch, e);
 }
 
 extern "C" int nf_linear_wgrad(int dtype, const void* x, const void* g, int M, int K, int N, void* scratch, size_t scratch_bytes, float* dw,
@@ -203,7 +292,8 @@ extern "C" int nf_linear_wgrad(int dtype, const void* x, const void* g, int M, i
     return NF_EINVAL;
   if (scratch_bytes < nf_linear_scratch_bytes(dtype, M, K, N)) return NF_ENOWS;
   const Epilogue e{nullptr, nullptr, NF_ACT_NONE, nullptr, dw, 1};
-  const int rc = dtype == NF_F32 ? gemm<float>(g, 1, N, x, 1, K, N, K, M, (float*)scratch, e) : gemm<bf16>(g, 1, N, x, 1, K, N, K, M, (float*)scratch, e);
+  const Product d = wgrad_of(M, K, N);
+  const int rc = dtype == NF_F32 ? product<float>(d, g, x, scratch, e) : product<bf16>(d, g, x, scratch, e);
   if (rc != NF_OK || !db) return rc;
   float* part = (float*)scratch;  // the product's partial sums have been read by now
   const dim3 grid(sum_blocks(M), (N + 31) / 32);

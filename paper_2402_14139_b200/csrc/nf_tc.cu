@@ -3102,6 +3102,18 @@ int nf_tc_out_map(CUtensorMap* m, void* base, int N, int H, int W, int C, int BW
   return make_map4(m, base, d, b);
 }
 
+int nf_tc_map3(CUtensorMap* m, const void* base, bool f32, size_t inner, size_t outer, size_t planes, size_t row_bytes, size_t plane_bytes,
+               int box_rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return NF_ECUDA;
+  const cuuint64_t dims[3] = {inner, outer, planes}, strides[2] = {row_bytes, plane_bytes};
+  const cuuint32_t box[3] = {f32 ? 32u : 64u, (cuuint32_t)box_rows, 1}, es[3] = {1, 1, 1};
+  const CUresult r = fn(m, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, es,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? NF_OK : nf_cuda_check(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
+}
+
 static __device__ int32_t g_op_status;  // status word of the stand-alone operations (one per device that loads the library)
 
 int nf_tc_op_status_ptr(int32_t** out) {

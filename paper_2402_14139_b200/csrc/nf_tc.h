@@ -57,6 +57,9 @@ int nf_tc_aux_dgrad_dy(nf_layer* L, double M);
 struct CUtensorMap_st;
 int nf_tc_sm_count();
 int nf_tc_tile(int H, int W, int* BW, int* BH);
+// {inner, outer, plane} map of bf16 or float rows, boxes of 128 bytes x `box_rows` rows with the 128-byte swizzle, zero fill outside
+int nf_tc_map3(CUtensorMap_st* m, const void* base, bool f32, size_t inner, size_t outer, size_t planes, size_t row_bytes, size_t plane_bytes,
+               int box_rows);
 int nf_tc_out_map(CUtensorMap_st* m, void* base, int N, int H, int W, int C, int BW, int BH);
 // First layer in evaluation (nf_first.cu): act = ReLU(conv(x) * scale + shift) of `count` RGB images, from the images as they are.
 bool nf_first_eval_ok(const nf_layer* L, const void* x, int count, const void* act);

@@ -18,6 +18,7 @@ SHAPES = [  # M, K, N
     (1, 1, 1), (1, 8, 8), (1, 4096, 1000), (2, 2048, 10), (3, 64, 200), (5, 33, 7), (7, 512, 129), (8, 1024, 512), (16, 72, 64), (17, 520, 264), (33, 8, 1000),
     (64, 2048, 100), (100, 27, 64), (127, 129, 130), (128, 128, 128), (129, 256, 256), (200, 64, 8), (256, 1000, 96), (300, 264, 520), (511, 511, 511),
     (640, 2056, 264), (1000, 16, 1000), (1777, 256, 72), (2050, 40, 300), (4097, 64, 64), (9000, 24, 10),
+    (3600, 72, 1030), (1800, 2000, 2056), (1801, 2009, 2051), (20000, 128, 136),
 ]
 
 
