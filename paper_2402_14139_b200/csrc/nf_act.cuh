@@ -6,19 +6,27 @@
 
 static inline bool nf_act_ok(int act) { return act >= NF_ACT_NONE && act <= NF_ACT_GELU; }
 
-// 1 / (1 + e^-z).  With bf16 storage the fast exponential and division are used: their error, about 2^-21 (1 + |z|), is far below
-// the 2^-9 of the stored result.  fp32 storage keeps the full-precision functions.
+// 1 / (1 + e^-z).  With bf16 storage the approximate exponential and reciprocal are used: their error, about 2^-22 (1 + |z|) relative,
+// is far below the 2^-9 of the stored result.  fp32 storage keeps the full-precision functions.
 template <typename T>
 __device__ __forceinline__ float nf_sigmoid(float z) {
   if constexpr (std::is_same<T, float>::value) return 1.f / (1.f + expf(-z));
-  return __fdividef(1.f, 1.f + __expf(fminf(-z, 80.f)));  // the fast division returns 0 for divisors above 2^126: e^80 stays below
+  float e, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.4426950408889634f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));  // 0 where e is infinite
+  return r;
 }
 // Standard normal distribution function by erfc, which keeps the small values of the left tail
 __device__ __forceinline__ float nf_normal_cdf(float z) { return 0.5f * erfcf(z * -0.70710678118654752f); }
 
+__device__ __forceinline__ float nf_relu(float z) {  // a NaN stays one
+  float r;
+  asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(r) : "f"(z));
+  return r;
+}
 template <typename T>
 __device__ __forceinline__ float nf_act_value(float z, int act) {
-  if (act == NF_ACT_RELU) return z < 0.f ? 0.f : z;  // a NaN stays one
+  if (act == NF_ACT_RELU) return nf_relu(z);
   if (act == NF_ACT_SILU) return z * nf_sigmoid<T>(z);
   if (act == NF_ACT_GELU) return z * nf_normal_cdf(z);
   return z;
@@ -32,4 +40,11 @@ __device__ __forceinline__ float nf_act_grad(float z, int act) {
   }
   if (act == NF_ACT_GELU) return fmaf(z * 0.39894228040143268f, expf(-0.5f * z * z), nf_normal_cdf(z));
   return 1.f;
+}
+// dy act'(z); behind a closed ReLU 0 whatever dy was
+template <typename T>
+__device__ __forceinline__ float nf_act_dz(float z, float dy, int act) {
+  if (act == NF_ACT_NONE) return dy;
+  if (act == NF_ACT_RELU) return z > 0.f ? dy : 0.f;
+  return dy * nf_act_grad<T>(z, act);
 }

@@ -113,10 +113,10 @@ __global__ void __launch_bounds__(256) act_backward_kernel(const T* saved, const
     ld8(saved + i, s);
     ld8(dy + i, d);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) d[e] *= nf_act_grad<T>(s[e], act);
+    for (int e = 0; e < 8; ++e) d[e] = nf_act_dz<T>(s[e], d[e], act);
     st8(g + i, d);
   } else {
-    for (size_t e = i; e < n; ++e) stf(g, e, ldf(dy, e) * nf_act_grad<T>(ldf(saved, e), act));
+    for (size_t e = i; e < n; ++e) stf(g, e, nf_act_dz<T>(ldf(saved, e), ldf(dy, e), act));
   }
 }
 

@@ -4,17 +4,21 @@
 //   dz = dy act'(z);  dgamma = sum dz xh, dbeta = sum dz;
 //   dx = rstd (gamma dz - m1 - xh m2),  m1, m2 = means over the group of gamma dz and gamma dz xh
 //
-// One launch does a pass over the data for the sums and a second one for the result.  A cluster of CS blocks owns one image (or one
-// slice of its channels, whole groups), each block a range of its pixels; the blocks' channel sums meet through distributed
-// shared memory, and the second pass finds the image in L2, so that HBM carries every tensor once.
+// HBM has to carry every tensor once; the two passes over an image that the formulas need have to find it on the chip.  Two forms:
+//  - where a pixel of the slice (some whole groups) is a power of two of 16-byte pieces: teams of a warp up to clusters of sixteen blocks hold a
+//    slice in shared memory, and fill each place anew as soon as the second pass has read it, so that copies run under both passes.
+//  - any other shape: a cluster of blocks reads its slice twice, the second time from L2.
+// Parameter gradients gather in registers or shared memory over all images of a team or block, then in one row of partials each.
 //
-// Sums: a thread adds in fp32 what it sees of its channels, after subtracting the image's first pixel of the channel (forward), so that
-// a mean far from zero costs no digits; blocks, ranks and the channels of a group are joined in fp64.  xh and z are formed by
-// separately rounded operations in this order in both directions, so that the gradient's ReLU mask is the forward's.
+// Sums: a thread adds in fp32 what it sees of its channels, in the forward pass after subtracting a value of the group or channel, so that a mean far from zero costs no digits; ranges of pixels are joined by their means and squared deviations.  xh and z
+// are formed by separately rounded operations in this order in both directions, so that the gradient's ReLU mask is the forward's.
 #include <cooperative_groups.h>
+
+#include <cuda.h>
 
 #include "nf_act.cuh"
 #include "nf_ldst.cuh"
+#include "nf_ptx.cuh"
 #include "nf_tc.h"
 
 namespace {
@@ -23,7 +27,7 @@ namespace cg = cooperative_groups;
 constexpr int kNT = 256;
 constexpr int kMaxCs = 4096;       // channels of a slice: totals of all of them lie in shared memory
 constexpr int kMaxCluster = 16;    // above 8 is outside the portable limit and has to be allowed per kernel
-constexpr int kMaxParts = 1184;    // rows of dgamma / dbeta partials at most: 8 blocks on each of 148 SMs
+constexpr int kMaxBlocks = 1184;   // persistent blocks at most (rows of dgamma / dbeta partials): 8 on each of 148 SMs
 
 struct GnArgs {
   const void *x, *dy;
@@ -33,42 +37,128 @@ struct GnArgs {
   float* part;         // backward: [rows][2][C] partial sums of dbeta, dgamma
   int N, P, C, G, cpg;
   int slices, Cs, vpr;  // channel slices, channels and vectors per slice
-  int CS, stride;       // blocks per cluster; images between two turns of a cluster
+  int CS, stride;       // blocks per cluster; images between two turns of a cluster or team
+  int TS;               // threads of a team
+  int rpc, hold, buffers;  // held form: pixels per block; pieces per thread and tensor; images in shared memory at a time
+  int32_t* status;
   int act;
   float eps;
 };
 
+// V values of storage type T as loaded (16 bytes, or one value), and as pairs of floats
+template <typename T, int V> struct Raw;
+template <> struct Raw<bf16, 8> {
+  uint4 u;
+  __device__ __forceinline__ void load(const bf16* p) { u = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void load_last(const bf16* p) { u = __ldcs(reinterpret_cast<const uint4*>(p)); }
+  __device__ __forceinline__ void load_shared(uint32_t at) { u = ptx::lds128(at); }
+  __device__ __forceinline__ f32x2 pair(int i) const {
+    const uint32_t w = i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w;
+    return nf_pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+  }
+};
+template <> struct Raw<float, 4> {
+  float4 u;
+  __device__ __forceinline__ void load(const float* p) { u = *reinterpret_cast<const float4*>(p); }
+  __device__ __forceinline__ void load_last(const float* p) { u = __ldcs(reinterpret_cast<const float4*>(p)); }
+  __device__ __forceinline__ void load_shared(uint32_t at) {
+    const uint4 w = ptx::lds128(at);
+    u = make_float4(__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w));
+  }
+  __device__ __forceinline__ f32x2 pair(int i) const { return i == 0 ? nf_pack2(u.x, u.y) : nf_pack2(u.z, u.w); }
+};
+template <typename T> struct Raw<T, 1> {
+  float u;
+  __device__ __forceinline__ void load(const T* p) { u = ldf(p, 0); }
+  __device__ __forceinline__ void load_last(const T* p) { u = ldf(p, 0); }
+  __device__ __forceinline__ f32x2 pair(int) const { return nf_pack2(u, 0.f); }
+};
 template <typename T, int V>
-__device__ __forceinline__ void ldv(const T* p, float (&v)[V]) {
-  if constexpr (V == 8) {
-    ld8(p, v);
-  } else if constexpr (V == 4 && std::is_same<T, float>::value) {
-    const float4 a = *reinterpret_cast<const float4*>(p);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-  } else {
+__device__ __forceinline__ void store(T* p, const f32x2 (&v)[(V + 1) / 2]) {
+  float f[V + 1];
 #pragma unroll
-    for (int e = 0; e < V; ++e) v[e] = ldf(p, e);
+  for (int i = 0; i < (V + 1) / 2; ++i) nf_unpack2(v[i], f[2 * i], f[2 * i + 1]);
+  if constexpr (V == 8) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 b = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&b);
+    }
+    __stcs(reinterpret_cast<uint4*>(p), make_uint4(w[0], w[1], w[2], w[3]));
+  } else if constexpr (V == 4) {
+    __stcs(reinterpret_cast<float4*>(p), make_float4(f[0], f[1], f[2], f[3]));
+  } else {
+    stf(p, 0, f[0]);
   }
 }
-template <typename T, int V>
-__device__ __forceinline__ void stv(T* p, float (&v)[V]) {
-  if constexpr (V == 8) {
-    st8(p, v);
-  } else if constexpr (V == 4 && std::is_same<T, float>::value) {
-    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-  } else {
-#pragma unroll
-    for (int e = 0; e < V; ++e) stf(p, e, v[e]);
+__device__ __forceinline__ f32x2 both(float v) { return nf_pack2(v, v); }
+__device__ __forceinline__ float low(f32x2 v) { float a, b; nf_unpack2(v, a, b); return a; }
+__device__ __forceinline__ float high(f32x2 v) { float a, b; nf_unpack2(v, a, b); return b; }
+
+// ACT: an nf_act known to the compiler, or kAnyAct: `act` says
+constexpr int kAnyAct = -1;
+template <typename T, int ACT>
+__device__ __forceinline__ f32x2 act2(f32x2 z, int act) {
+  if constexpr (ACT == NF_ACT_NONE) return z;
+  float a, b;
+  nf_unpack2(z, a, b);
+  return nf_pack2(nf_act_value<T>(a, ACT == kAnyAct ? act : ACT), nf_act_value<T>(b, ACT == kAnyAct ? act : ACT));
+}
+// dz = dy act'(z)
+template <typename T, int ACT>
+__device__ __forceinline__ f32x2 grad2(f32x2 z, f32x2 dy, int act) {
+  if constexpr (ACT == NF_ACT_NONE) return dy;
+  float a, b;
+  nf_unpack2(z, a, b);
+  if constexpr (ACT == NF_ACT_RELU) {
+    float c, d;
+    nf_unpack2(dy, c, d);
+    return nf_pack2(a > 0.f ? c : 0.f, b > 0.f ? d : 0.f);
   }
+  if constexpr (ACT == NF_ACT_SILU) {  // s (1 + z (1 - s))
+    const f32x2 s = nf_pack2(nf_sigmoid<T>(a), nf_sigmoid<T>(b));
+    const f32x2 t = nf_fma2(nf_mul2(z, s), nf_fma2(s, both(-1.f), both(1.f)), s);
+    return nf_mul2(t, dy);
+  }
+  float c, d;
+  nf_unpack2(dy, c, d);
+  return nf_pack2(nf_act_dz<T>(a, c, ACT == kAnyAct ? act : ACT), nf_act_dz<T>(b, d, ACT == kAnyAct ? act : ACT));
 }
 
-__device__ __forceinline__ float normalised(float x, float mean, float rstd) { return __fmul_rn(__fsub_rn(x, mean), rstd); }
-__device__ __forceinline__ float affine(float xh, float g, float b) { return __fadd_rn(__fmul_rn(xh, g), b); }
+// Parameters of a thread's V channels, as pairs.  ONE: they belong to one group
+template <int V, bool ONE = false>
+struct Chan {
+  static constexpr int NP = (V + 1) / 2, NS = ONE ? 1 : NP;
+  f32x2 nmu[NS], rs[NS], ga[NP], be[NP];
+  __device__ __forceinline__ void affine(const GnArgs& a, int c) {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int d = V == 1 ? c : c + 2 * i + 1;
+      ga[i] = nf_pack2(a.gamma[c + 2 * i], a.gamma[d]);
+      be[i] = nf_pack2(a.beta[c + 2 * i], a.beta[d]);
+    }
+  }
+  template <typename F>
+  __device__ __forceinline__ void stats(int c, int cpg, F&& at) {  // at(group) -> (mean, rstd)
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      const float2 p = at((c + 2 * i) / cpg), q = V == 1 || ONE ? p : at((c + 2 * i + 1) / cpg);
+      nmu[i] = nf_pack2(-p.x, -q.x);
+      rs[i] = nf_pack2(p.y, q.y);
+    }
+  }
+  __device__ __forceinline__ f32x2 scale(int i) const { return rs[ONE ? 0 : i]; }
+  __device__ __forceinline__ f32x2 xh(f32x2 x, int i) const { return nf_mul2(nf_add2(x, nmu[ONE ? 0 : i]), rs[ONE ? 0 : i]); }
+  __device__ __forceinline__ f32x2 z(f32x2 xh, int i) const { return nf_add2(nf_mul2(xh, ga[i]), be[i]); }
+};
 
+// ---------------------------------------------------------------- large images
 // V channels per thread; threads run along the channels of a pixel first, then along the pixels
-template <typename T, int V, bool BWD>
-__global__ void __launch_bounds__(kNT) group_norm_kernel(const GnArgs a) {
+template <typename T, int V, int ACT, bool BWD>
+__global__ void __launch_bounds__(kNT, 2) group_norm_kernel(const GnArgs a) {
   nf_pdl_begin();
+  constexpr int NP = (V + 1) / 2, U = BWD ? 4 : 8;  // loads in flight per thread and tensor
   extern __shared__ __align__(16) float sm[];
   float* red = sm;                        // [2V][kNT] tree reduction
   float* tot = red + 2 * V * kNT;         // [2][2][Cs] this block's channel sums, two images in turn
@@ -85,66 +175,77 @@ __global__ void __launch_bounds__(kNT) group_norm_kernel(const GnArgs a) {
   const T* x = (const T*)a.x;
   const T* dy = (const T*)a.dy;
   T* out = (T*)a.out;
+  const bool one_col = a.vpr <= kNT;  // a thread's channels stay the same
+  Chan<V> ch;
+  if (one_col && on) ch.affine(a, c0 + tc * V);
   if constexpr (BWD) {
     for (int i = threadIdx.x; i < 2 * a.Cs; i += kNT) acc[i] = 0.f;
   }
   int turn = 0;
   for (int n = cid / a.slices; n < a.N; n += a.stride, turn ^= 1) {
     const size_t base = (size_t)n * a.P * a.C + c0;
+    const size_t gbase = (size_t)n * a.G + slice * gps;
     float* mine = tot + turn * 2 * a.Cs;
+    auto saved = [&](int g) { return make_float2(a.mean[gbase + g], a.rstd[gbase + g]); };
     for (int cv0 = 0; cv0 < a.vpr; cv0 += cols) {
       const int cv = cv0 + tc;
-      const bool here = on && cv < a.vpr;
-      float s[V], q[V];
+      f32x2 s[NP], q[NP];
 #pragma unroll
-      for (int e = 0; e < V; ++e) s[e] = q[e] = 0.f;
-      if (here) {
+      for (int i = 0; i < NP; ++i) s[i] = q[i] = 0;
+      if (on && cv < a.vpr) {
         const size_t col = base + (size_t)cv * V;
-        if constexpr (!BWD) {
-          float k[V];
-          ldv<T, V>(x + col, k);
-#pragma unroll 4
-          for (int p = p0 + tr; p < p1; p += R) {
-            float v[V];
-            ldv<T, V>(x + col + (size_t)p * a.C, v);
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-              const float d = v[e] - k[e];
-              s[e] += d;
-              q[e] = fmaf(d, d, q[e]);
-            }
-          }
+        f32x2 nk[NP];  // forward: minus the pivots
+        if constexpr (BWD) {
+          if (!one_col) ch.affine(a, c0 + cv * V);
+          ch.stats(cv * V, a.cpg, saved);
         } else {
-          float mu[V], rs[V], ga[V], be[V];
+          Raw<T, V> k;
+          k.load(x + col);
 #pragma unroll
-          for (int e = 0; e < V; ++e) {
-            const int c = c0 + cv * V + e;
-            mu[e] = a.mean[(size_t)n * a.G + c / a.cpg];
-            rs[e] = a.rstd[(size_t)n * a.G + c / a.cpg];
-            ga[e] = a.gamma[c];
-            be[e] = a.beta[c];
-          }
-#pragma unroll 2
-          for (int p = p0 + tr; p < p1; p += R) {
-            float v[V], g[V];
-            ldv<T, V>(x + col + (size_t)p * a.C, v);
-            ldv<T, V>(dy + col + (size_t)p * a.C, g);
+          for (int i = 0; i < NP; ++i) nk[i] = nf_mul2(k.pair(i), both(-1.f));
+        }
+        auto add = [&](const Raw<T, V>& v, const Raw<T, V>& g) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-              const float xh = normalised(v[e], mu[e], rs[e]);
-              const float dz = g[e] * nf_act_grad<T>(affine(xh, ga[e], be[e]), a.act);
-              s[e] += dz;
-              q[e] = fmaf(dz, xh, q[e]);
+          for (int i = 0; i < NP; ++i) {
+            if constexpr (BWD) {
+              const f32x2 xh = ch.xh(v.pair(i), i);
+              const f32x2 dz = grad2<T, ACT>(ACT == NF_ACT_NONE ? xh : ch.z(xh, i), g.pair(i), a.act);
+              s[i] = nf_add2(s[i], dz);
+              q[i] = nf_fma2(dz, xh, q[i]);
+            } else {
+              const f32x2 d = nf_add2(v.pair(i), nk[i]);
+              s[i] = nf_add2(s[i], d);
+              q[i] = nf_fma2(d, d, q[i]);
             }
           }
+        };
+        int p = p0 + tr;
+        const size_t step = (size_t)R * a.C;
+        size_t at = col + (size_t)p * a.C;
+        for (; p + (U - 1) * R < p1; p += U * R, at += U * step) {
+          Raw<T, V> v[U], g[BWD ? U : 1];
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            v[u].load(x + at + u * step);
+            if constexpr (BWD) g[u].load(dy + at + u * step);
+          }
+#pragma unroll
+          for (int u = 0; u < U; ++u) add(v[u], g[BWD ? u : 0]);
+        }
+        for (; p < p1; p += R, at += step) {
+          Raw<T, V> v, g;
+          v.load(x + at);
+          if constexpr (BWD) g.load(dy + at);
+          else g = v;
+          add(v, g);
         }
       }
       // rows of threads are folded in halves
       __syncthreads();
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        red[e * kNT + threadIdx.x] = s[e];
-        red[(V + e) * kNT + threadIdx.x] = q[e];
+      for (int i = 0; i < V; ++i) {
+        red[i * kNT + threadIdx.x] = i % 2 ? high(s[i / 2]) : low(s[i / 2]);
+        red[(V + i) * kNT + threadIdx.x] = i % 2 ? high(q[i / 2]) : low(q[i / 2]);
       }
       for (int left = R; left > 1;) {
         const int half = (left + 1) / 2;
@@ -175,6 +276,7 @@ __global__ void __launch_bounds__(kNT) group_norm_kernel(const GnArgs a) {
           for (int i = lane; i < a.cpg; i += L) {
             const int c = g * a.cpg + i;
             double S = 0, Q = 0;
+#pragma unroll 4
             for (int r = 0; r < a.CS; ++r) {
               const float* o = cluster.map_shared_rank(mine, r);
               S += o[c];
@@ -202,8 +304,8 @@ __global__ void __launch_bounds__(kNT) group_norm_kernel(const GnArgs a) {
             gsm[g] = mf;
             gsm[gps + g] = rf;
             if (rank == 0) {
-              a.mean[(size_t)n * a.G + slice * gps + g] = mf;
-              a.rstd[(size_t)n * a.G + slice * gps + g] = rf;
+              a.mean[gbase + g] = mf;
+              a.rstd[gbase + g] = rf;
             }
           } else {
             const double M = (double)a.cpg * a.P;
@@ -219,42 +321,53 @@ __global__ void __launch_bounds__(kNT) group_norm_kernel(const GnArgs a) {
     __syncthreads();
     for (int cv = tc; on && cv < a.vpr; cv += cols) {
       const size_t col = base + (size_t)cv * V;
-      float mu[V], rs[V], ga[V], be[V];
-      float m1[BWD ? V : 1], m2[BWD ? V : 1];
+      f32x2 m1[NP], m2[NP];
+      if (!one_col) ch.affine(a, c0 + cv * V);
+      if constexpr (!BWD) {
+        ch.stats(cv * V, a.cpg, [&](int g) { return make_float2(gsm[g], gsm[gps + g]); });
+      } else {
+        if (!one_col) ch.stats(cv * V, a.cpg, saved);
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const int c = cv * V + e, g = c / a.cpg;
-        ga[e] = a.gamma[c0 + c];
-        be[e] = a.beta[c0 + c];
-        if constexpr (!BWD) {
-          mu[e] = gsm[g];
-          rs[e] = gsm[gps + g];
-        } else {
-          mu[e] = a.mean[(size_t)n * a.G + slice * gps + g];
-          rs[e] = a.rstd[(size_t)n * a.G + slice * gps + g];
-          m1[e] = gsm[g];
-          m2[e] = gsm[gps + g];
+        for (int i = 0; i < NP; ++i) {
+          const int g = (cv * V + 2 * i) / a.cpg, h = V == 1 ? g : (cv * V + 2 * i + 1) / a.cpg;
+          m1[i] = nf_pack2(-gsm[g], -gsm[h]);
+          m2[i] = nf_pack2(-gsm[gps + g], -gsm[gps + h]);
         }
       }
-#pragma unroll 2
-      for (int p = p0 + tr; p < p1; p += R) {
-        const size_t at = col + (size_t)p * a.C;
-        float v[V];
-        ldv<T, V>(x + at, v);
-        if constexpr (!BWD) {
+      auto result = [&](const Raw<T, V>& v, const Raw<T, V>& g, T* to) {
+        f32x2 o[NP];
 #pragma unroll
-          for (int e = 0; e < V; ++e) v[e] = nf_act_value<T>(affine(normalised(v[e], mu[e], rs[e]), ga[e], be[e]), a.act);
-        } else {
-          float g[V];
-          ldv<T, V>(dy + at, g);
-#pragma unroll
-          for (int e = 0; e < V; ++e) {
-            const float xh = normalised(v[e], mu[e], rs[e]);
-            const float dz = g[e] * nf_act_grad<T>(affine(xh, ga[e], be[e]), a.act);
-            v[e] = rs[e] * (fmaf(ga[e], dz, -m1[e]) - xh * m2[e]);
+        for (int i = 0; i < NP; ++i) {
+          const f32x2 xh = ch.xh(v.pair(i), i);
+          if constexpr (BWD) {
+            const f32x2 dz = grad2<T, ACT>(ACT == NF_ACT_NONE ? xh : ch.z(xh, i), g.pair(i), a.act);
+            o[i] = nf_mul2(ch.scale(i), nf_fma2(xh, m2[i], nf_fma2(ch.ga[i], dz, m1[i])));
+          } else {
+            o[i] = act2<T, ACT>(ch.z(xh, i), a.act);
           }
         }
-        stv<T, V>(out + at, v);
+        store<T, V>(to, o);
+      };
+      constexpr int W = BWD ? 4 : 8;
+      int p = p0 + tr;
+      const size_t step = (size_t)R * a.C;
+      size_t at = col + (size_t)p * a.C;
+      for (; p + (W - 1) * R < p1; p += W * R, at += W * step) {
+        Raw<T, V> v[W], g[BWD ? W : 1];
+#pragma unroll
+        for (int u = 0; u < W; ++u) {
+          v[u].load_last(x + at + u * step);
+          if constexpr (BWD) g[u].load_last(dy + at + u * step);
+        }
+#pragma unroll
+        for (int u = 0; u < W; ++u) result(v[u], g[BWD ? u : 0], out + at + u * step);
+      }
+      for (; p < p1; p += R, at += step) {
+        Raw<T, V> v, g;
+        v.load_last(x + at);
+        if constexpr (BWD) g.load_last(dy + at);
+        else g = v;
+        result(v, g, out + at);
       }
     }
   }
@@ -269,40 +382,537 @@ __global__ void __launch_bounds__(kNT) group_norm_kernel(const GnArgs a) {
   cluster.sync();  // no block leaves while another may still read its sums
 }
 
-// dbeta, dgamma: the rows of partials added in fp64, eight chains of every eighth row, joined in order
-__global__ void __launch_bounds__(256) group_norm_param_kernel(const float* __restrict__ part, int rows, int C, float* __restrict__ dgamma,
-                                                               float* __restrict__ dbeta) {
+// ---------------------------------------------------------------- slices held in shared memory
+// A team of TS threads works on one image's slice (in a cluster: each block's team on a range of its pixels).  A slice is `vpr` 16-byte pieces
+// of a pixel, a power of two up to 32, whole groups; a thread takes pieces t, t + TS, ..., so its channels stay the same, and it alone
+// copies them into shared memory (cp.async), reads them in both passes and refills their places with the image `buffers` turns on: no
+// barrier guards the data.  Sums of a group: shuffles; teams of several warps add one number per warp and group through shared memory; blocks of a
+// cluster send theirs to each other (st.async into slots of the receiver, counted by its barrier).  FINE: groups of fewer channels than a piece;
+// MORE: the slice is larger than what is held.
+constexpr int kSlotGroups = 64;
+
+__device__ __forceinline__ void copy16(uint32_t to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void copies_wait(int behind) {  // all but the latest `behind` groups have landed
+  if (behind <= 0) asm volatile("cp.async.wait_group 0;" ::: "memory");
+  else if (behind == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
+  else if (behind == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
+  else asm volatile("cp.async.wait_group 3;" ::: "memory");
+}
+
+template <typename T, int V, int ACT, bool BWD, bool FINE, int NT, bool MORE>
+__global__ void __launch_bounds__(NT, 512 / NT) group_norm_held_kernel(const GnArgs a) {
+  constexpr int NP = V / 2, S = FINE ? V : 1, kTensors = BWD ? 2 : 1;
+  extern __shared__ __align__(16) uint8_t held_raw[];
+  __shared__ float part[NT / 32][2][kSlotGroups];        // per warp: totals of the slots (groups, or FINE channels)
+  __shared__ float2 gsm[NT / 32 * 32];                  // per team: mean and rstd, or m1 and m2
+  __shared__ float2 peers[2][kMaxCluster][32];          // the blocks' totals, two items in turn
+  __shared__ uint64_t xbar[2];
+  __shared__ int abort_word;
+  const int TS = a.TS, team = threadIdx.x / TS, t = threadIdx.x % TS, lane = threadIdx.x & 31, warps = TS / 32;
+  const int rank = blockIdx.x % a.CS, id = blockIdx.x / a.CS * (NT / TS) + team, slice = id % a.slices;
+  const int tc = t % a.vpr, tr = t / a.vpr, rows = TS / a.vpr;
+  const int gps = a.Cs / a.cpg, c0 = slice * a.Cs;
+  const int lo = a.cpg > V ? a.cpg / V : 1;
+  const int p0 = rank * a.rpc, np = max(0, min(a.P - p0, a.rpc));
+  // Turns over the slice: `whole` of them with a piece for every thread, then one where some have none.  The first a.hold are held; the rest of
+  // a very large image (MORE) is read again, from L2.
+  const int whole = np * a.vpr / TS, kw = min(whole, a.hold);
+  const bool last = t < np * a.vpr - whole * TS, last_held = last && whole < a.hold;
+  if (a.CS > 1) {
+    if (threadIdx.x == 0) {
+      ptx::mbar_init(&xbar[0], 1);
+      ptx::mbar_init(&xbar[1], 1);
+      abort_word = 0;
+      ptx::fence_mbar_init();
+    }
+    __syncthreads();
+    ptx::cluster_sync();
+  }
   nf_pdl_begin();
-  __shared__ double sm[8][32];
-  const int tx = threadIdx.x % 32, ty = threadIdx.x / 32;
-  const int i = blockIdx.x * 32 + tx;
-  double s = 0;
-  if (i < 2 * C)
-    for (int r = ty; r < rows; r += 8) s += part[(size_t)r * 2 * C + i];
-  sm[ty][tx] = s;
-  __syncthreads();
-  if (ty == 0 && i < 2 * C) {
-    for (int k = 1; k < 8; ++k) s += sm[k][tx];
-    (i < C ? dbeta[i] : dgamma[i - C]) = (float)s;
+
+  const T* x = (const T*)a.x + (size_t)p0 * a.C + c0 + tc * V;
+  const T* dy = (const T*)a.dy + (size_t)p0 * a.C + c0 + tc * V;
+  T* out = (T*)a.out + (size_t)p0 * a.C + c0 + tc * V;
+  const size_t image = (size_t)a.P * a.C, row_step = (size_t)rows * a.C;
+  constexpr uint32_t kstep = NT * 16;
+  const uint32_t slot0 = ptx::smem_u32(held_raw) + threadIdx.x * 16, tstep = a.hold * kstep, bstep = kTensors * tstep;
+  const int first = id / a.slices;
+  for (int i = 0; i < a.buffers; ++i) {
+    const int n = first + i * a.stride;
+    if (n < a.N) {
+      size_t at = (size_t)n * image + (size_t)tr * a.C;
+      uint32_t slot = slot0 + i * bstep;
+      for (int k = 0; k < kw + last_held; ++k, at += row_step, slot += kstep) {
+        copy16(slot, x + at);
+        if constexpr (BWD) copy16(slot + tstep, dy + at);
+      }
+    }
+    copies_end();
+  }
+  Chan<V, !FINE> ch;
+  constexpr int NS = FINE ? NP : 1;
+  ch.affine(a, c0 + tc * V);
+  f32x2 db[NP], dg[NP];
+#pragma unroll
+  for (int i = 0; i < NP; ++i) db[i] = dg[i] = 0;
+
+  // Read one image ahead: its statistics (backward), or the pivot of this thread's group, the group's first channel at the block's first pixel
+  float2 ahead = make_float2(0.f, 0.f);
+  const int pivot_at = (p0 < a.P ? p0 : a.P - 1) * a.C + c0 + tc / lo * a.cpg;
+  auto look = [&](int n) {
+    if (FINE || n >= a.N) return;
+    if constexpr (BWD) {
+      const size_t g = (size_t)n * a.G + slice * gps + tc / lo;
+      ahead = make_float2(a.mean[g], a.rstd[g]);
+    } else {
+      ahead.x = ldf((const T*)a.x, (size_t)n * image + pivot_at);
+    }
+  };
+  look(first);
+  int b = 0, turn = 0;
+  uint32_t xph = 0;
+  for (int n = first; n < a.N; n += a.stride) {
+    const size_t gbase = (size_t)n * a.G + slice * gps;
+    const uint32_t slot = slot0 + b * bstep;
+    f32x2 nk[BWD ? 1 : NS];
+    float pivot[S];
+    if constexpr (BWD) {
+      if constexpr (FINE) ch.stats(tc * V, a.cpg, [&](int i) { return make_float2(a.mean[gbase + i], a.rstd[gbase + i]); });
+      else ch.stats(0, 1, [&](int) { return ahead; });
+    } else {
+      if constexpr (FINE) {
+        const T* px = (const T*)a.x + (size_t)n * image + (size_t)(p0 < a.P ? p0 : a.P - 1) * a.C + c0;
+#pragma unroll
+        for (int i = 0; i < V; ++i) pivot[i] = ldf(px, (tc * V + i) / a.cpg * a.cpg);
+      } else {
+        pivot[0] = ahead.x;
+      }
+#pragma unroll
+      for (int i = 0; i < NS; ++i) nk[i] = nf_pack2(-pivot[FINE ? 2 * i : 0], -pivot[FINE ? 2 * i + 1 : 0]);
+    }
+    look(n + a.stride);
+    f32x2 s[NP], q[NP];
+#pragma unroll
+    for (int i = 0; i < NP; ++i) s[i] = q[i] = 0;
+    auto add = [&](const Raw<T, V>& v, const Raw<T, V>& g) {
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        if constexpr (BWD) {
+          const f32x2 xh = ch.xh(v.pair(i), i);
+          const f32x2 dz = grad2<T, ACT>(ACT == NF_ACT_NONE ? xh : ch.z(xh, i), g.pair(i), a.act);
+          s[i] = nf_add2(s[i], dz);
+          q[i] = nf_fma2(dz, xh, q[i]);
+        } else {
+          const f32x2 d = nf_add2(v.pair(i), nk[FINE ? i : 0]);
+          s[i] = nf_add2(s[i], d);
+          q[i] = nf_fma2(d, d, q[i]);
+        }
+      }
+    };
+    const size_t own_at = (size_t)n * image + (size_t)tr * a.C;  // this thread's first piece
+    constexpr int U = BWD ? 2 : 4;  // pieces of a very large image in flight per thread and tensor
+    if constexpr (MORE) {
+      size_t at = own_at + a.hold * row_step;
+      int left = whole - a.hold;
+      for (; left >= U; left -= U) {
+        Raw<T, V> v[U], g[BWD ? U : 1];
+#pragma unroll
+        for (int u = 0; u < U; ++u, at += row_step) {
+          v[u].load(x + at);
+          if constexpr (BWD) g[u].load(dy + at);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) add(v[u], g[BWD ? u : 0]);
+      }
+      for (left += last; left > 0; --left, at += row_step) {
+        Raw<T, V> v, g;
+        v.load(x + at);
+        if constexpr (BWD) g.load(dy + at);
+        else g = v;
+        add(v, g);
+      }
+    }
+    copies_wait(a.buffers - 1);
+    {
+      auto one = [&](uint32_t at) {
+        Raw<T, V> v, g;
+        v.load_shared(at);
+        if constexpr (BWD) g.load_shared(at + tstep);
+        else g = v;
+        add(v, g);
+      };
+      uint32_t at = slot;
+      int k = kw;
+      for (; k >= 4; k -= 4, at += 4 * kstep) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) one(at + u * kstep);
+      }
+      for (k += last_held; k > 0; --k, at += kstep) one(at);
+    }
+    if constexpr (BWD) {
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        db[i] = nf_add2(db[i], s[i]);
+        dg[i] = nf_add2(dg[i], q[i]);
+        s[i] = nf_mul2(s[i], ch.ga[i]);
+        q[i] = nf_mul2(q[i], ch.ga[i]);
+      }
+    }
+    float f[2][S];
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      float v[V];
+#pragma unroll
+      for (int i = 0; i < NP; ++i) nf_unpack2(w ? q[i] : s[i], v[2 * i], v[2 * i + 1]);
+      if constexpr (FINE) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) f[w][i] = v[i];
+        // channels of a group lie next to each other in the thread
+        if (a.cpg >= 2) {
+#pragma unroll
+          for (int i = 0; i < S; i += 2) f[w][i] = f[w][i + 1 < S ? i + 1 : i] = f[w][i] + f[w][i + 1 < S ? i + 1 : i];
+        }
+        if (S == 8 && a.cpg >= 4) {
+#pragma unroll
+          for (int i = 0; i + 2 < S; i += 4) f[w][i] = f[w][i + 1] = f[w][i + 2] = f[w][i + 3] = f[w][i] + f[w][i + 2];
+        }
+      } else {
+        f[w][0] = v[0];
+#pragma unroll
+        for (int i = 1; i < V; ++i) f[w][0] += v[i];
+      }
+    }
+    // over the lanes that share the group
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2)
+      if (o < lo || o >= a.vpr) {
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+#pragma unroll
+          for (int i = 0; i < S; ++i) f[w][i] += __shfl_xor_sync(0xffffffffu, f[w][i], o);
+      }
+    const float M = (float)a.P * a.cpg;
+    // Group totals (A, B) of a block's pixels -> mean, squared deviations; statistics -> what pass two wants
+    auto about = [&](float& A, float& B, float k, int pixels) {
+      const float d = pixels ? A / ((float)pixels * a.cpg) : 0.f;  // counts are below 2^24: the pixels fit shared memory
+      B = fmaf(-A, d, B);
+      if (B < 0.f) B = 0.f;  // a NaN stays one
+      A = k + d;
+    };
+    float2 mine[S];
+    if (warps == 1) {
+#pragma unroll
+      for (int i = 0; i < S; ++i) {
+        if constexpr (BWD) {
+          mine[i] = make_float2(-f[0][i] / M, -f[1][i] / M);
+        } else {
+          about(f[0][i], f[1][i], pivot[i], np);
+          mine[i] = make_float2(f[0][i], 1.f / sqrtf(f[1][i] / M + a.eps));
+        }
+      }
+      if (!BWD && tr == 0 && tc % lo == 0) {
+#pragma unroll
+        for (int i = 0; i < S; ++i)
+          if (!FINE || i % a.cpg == 0) {
+            const int g = (tc * V + i) / a.cpg;
+            a.mean[gbase + g] = mine[i].x;
+            a.rstd[gbase + g] = mine[i].y;
+          }
+      }
+    } else {
+      if (lane < a.vpr && lane % lo == 0) {
+#pragma unroll
+        for (int i = 0; i < S; ++i)
+          if (!FINE || i % a.cpg == 0) {
+            const int g = (tc * V + i) / a.cpg;
+            part[threadIdx.x / 32][0][g] = f[0][i];
+            part[threadIdx.x / 32][1][g] = f[1][i];
+          }
+      }
+      ptx::named_barrier(1 + team, TS);
+      float2* own = gsm + team * warps * 32;  // up to 32 groups per warp of the team
+      // a warp per group: its lanes join the warps' sums (A in the lower half, B in the upper), then the other blocks'
+      for (int g = t / 32; g < gps; g += warps) {
+        const int w = lane & 15;
+        float v = w < warps ? part[team * warps + w][lane >> 4][g] : 0.f;
+        float k = 0.f;
+        if constexpr (!BWD) k = ldf((const T*)a.x, (size_t)n * image + (size_t)(p0 < a.P ? p0 : a.P - 1) * a.C + c0 + g * a.cpg);
+#pragma unroll
+        for (int o = 1; o < 16; o *= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
+        float A = __shfl_sync(0xffffffffu, v, 0), B = __shfl_sync(0xffffffffu, v, 16);
+        if constexpr (!BWD) about(A, B, k, np);
+        if (a.CS > 1) {
+          if (t == 0 && g == 0) ptx::mbar_expect_tx(&xbar[turn], a.CS * gps * 8);  // once: the barrier counts one arrival
+          if (lane < a.CS) ptx::st_async_f2(&peers[turn][rank][g], A, B, &xbar[turn], lane);
+        }
+        if (lane == 0) own[g] = make_float2(A, B);
+      }
+      __syncwarp();
+      for (int g = t / 32; g < gps; g += warps) {
+        float A = own[g].x, B = own[g].y;
+        if (a.CS > 1) {
+          if (g == t / 32) ptx::mbar_wait(&xbar[turn], (xph >> turn) & 1, &abort_word);  // sets the abort word itself when it gives up
+          const float2 from = lane < a.CS ? peers[turn][lane][g] : make_float2(0.f, 0.f);
+          const float cr = lane < a.CS ? (float)max(0, min(a.P - lane * a.rpc, a.rpc)) : 0.f;
+          const float base = __shfl_sync(0xffffffffu, from.x, 0);  // block 0 has pixels: means are joined by their distances from its mean
+          const float d = BWD ? from.x : cr > 0.f ? from.x - base : 0.f;
+          float m = BWD ? d : cr * d, M2 = from.y;
+#pragma unroll
+          for (int o = 1; o < kMaxCluster; o *= 2) m += __shfl_xor_sync(0xffffffffu, m, o);
+          if constexpr (!BWD) {
+            m /= (float)a.P;
+            M2 += cr * (float)a.cpg * (d - m) * (d - m);
+          }
+#pragma unroll
+          for (int o = 1; o < kMaxCluster; o *= 2) M2 += __shfl_xor_sync(0xffffffffu, M2, o);
+          A = BWD ? m : base + m;
+          B = M2;
+        }
+        if (lane == 0) {
+          if constexpr (BWD) {
+            own[g] = make_float2(-A / M, -B / M);
+          } else {
+            const float rf = 1.f / sqrtf(B / M + a.eps);
+            own[g] = make_float2(A, rf);
+            if (rank == 0) {
+              a.mean[gbase + g] = A;
+              a.rstd[gbase + g] = rf;
+            }
+          }
+        }
+      }
+      ptx::named_barrier(1 + team, TS);
+#pragma unroll
+      for (int i = 0; i < S; ++i) mine[i] = own[FINE ? (tc * V + i) / a.cpg : tc / lo];
+    }
+    if (a.CS > 1) xph ^= 1u << turn;
+    f32x2 m1[BWD ? NS : 1], m2[BWD ? NS : 1];
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      const float2 g = mine[FINE ? 2 * i : 0], h = mine[FINE ? 2 * i + 1 : 0];
+      if constexpr (BWD) {
+        m1[i] = nf_pack2(g.x, h.x);
+        m2[i] = nf_pack2(g.y, h.y);
+      } else {
+        ch.nmu[i] = nf_pack2(-g.x, -h.x);
+        ch.rs[i] = nf_pack2(g.y, h.y);
+      }
+    }
+    auto result = [&](const Raw<T, V>& v, const Raw<T, V>& g, T* to) {
+      f32x2 o[NP];
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        const f32x2 xh = ch.xh(v.pair(i), i);
+        if constexpr (BWD) {
+          const f32x2 dz = grad2<T, ACT>(ACT == NF_ACT_NONE ? xh : ch.z(xh, i), g.pair(i), a.act);
+          o[i] = nf_mul2(ch.scale(i), nf_fma2(xh, m2[FINE ? i : 0], nf_fma2(ch.ga[i], dz, m1[FINE ? i : 0])));
+        } else {
+          o[i] = act2<T, ACT>(ch.z(xh, i), a.act);
+        }
+      }
+      store<T, V>(to, o);
+    };
+    // Pass two; a place that has been read (the stored value depends on it) is filled with the image `buffers` turns on
+    auto held = [&](auto refill) {
+      constexpr bool kRefill = decltype(refill)::value;
+      T* to = out + own_at;
+      const size_t ahead_by = (size_t)a.buffers * a.stride * image;
+      const T* nx = x + own_at + ahead_by;
+      [[maybe_unused]] const T* nd = dy + own_at + ahead_by;
+      auto one = [&](uint32_t at) {
+        Raw<T, V> v, g;
+        v.load_shared(at);
+        if constexpr (BWD) g.load_shared(at + tstep);
+        else g = v;
+        result(v, g, to);
+        to += row_step;
+        if constexpr (kRefill) {
+          copy16(at, nx);
+          nx += row_step;
+          if constexpr (BWD) {
+            copy16(at + tstep, nd);
+            nd += row_step;
+          }
+        }
+      };
+      uint32_t at = slot;
+      int k = kw;
+      for (; k >= 4; k -= 4, at += 4 * kstep) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) one(at + u * kstep);
+      }
+      for (k += last_held; k > 0; --k, at += kstep) one(at);
+    };
+    if (n + a.buffers * a.stride < a.N) held(std::true_type());
+    else held(std::false_type());
+    if constexpr (MORE) {
+      size_t at = own_at + a.hold * row_step;
+      int left = whole - a.hold;
+      for (; left >= U; left -= U) {
+        Raw<T, V> v[U], g[BWD ? U : 1];
+        size_t from = at;
+#pragma unroll
+        for (int u = 0; u < U; ++u, from += row_step) {
+          v[u].load_last(x + from);
+          if constexpr (BWD) g[u].load_last(dy + from);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u, at += row_step) result(v[u], g[BWD ? u : 0], out + at);
+      }
+      for (left += last; left > 0; --left, at += row_step) {
+        Raw<T, V> v, g;
+        v.load_last(x + at);
+        if constexpr (BWD) g.load_last(dy + at);
+        else g = v;
+        result(v, g, out + at);
+      }
+    }
+    copies_end();
+    if (++b == a.buffers) b = 0;
+    turn ^= 1;
+  }
+  copies_wait(0);
+  if constexpr (BWD) {  // the team's rows of threads folded in halves; a row of partials per team and rank
+    float* sm = reinterpret_cast<float*>(held_raw);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      sm[i * NT + threadIdx.x] = i % 2 ? high(db[i / 2]) : low(db[i / 2]);
+      sm[(V + i) * NT + threadIdx.x] = i % 2 ? high(dg[i / 2]) : low(dg[i / 2]);
+    }
+    for (int left = TS / 2; left >= a.vpr; left /= 2) {
+      __syncthreads();
+      if (t < left) {
+#pragma unroll
+        for (int e = 0; e < 2 * V; ++e) sm[e * NT + threadIdx.x] += sm[e * NT + threadIdx.x + left];
+      }
+    }
+    __syncthreads();
+    float* row = a.part + (size_t)(id / a.slices * a.CS + rank) * 2 * a.C + c0;
+    for (int i = t; i < 2 * a.Cs; i += TS) {
+      const int w = i / a.Cs, c = i - w * a.Cs;
+      row[(size_t)w * a.C + c] = sm[(w * V + c % V) * NT + team * TS + c / V];
+    }
+  }
+  if (a.CS > 1) {
+    __syncthreads();
+    if (threadIdx.x == 0 && abort_word) atomicOr(a.status, NF_ETIMEOUT);
+    __syncwarp();
+    ptx::cluster_sync();  // no block leaves while another may still send it sums
   }
 }
 
+// dbeta, dgamma: the rows of partials added in fp64, 32 chains of every 32nd row, joined in order
+__global__ void __launch_bounds__(1024) group_norm_param_kernel(const float* __restrict__ part, int rows, int C, float* __restrict__ dgamma,
+                                                                float* __restrict__ dbeta) {
+  nf_pdl_begin();
+  __shared__ double sm[32][33];
+  const int tx = threadIdx.x % 32, ty = threadIdx.x / 32;
+  const int i = blockIdx.x * 32 + tx;
+  double s = 0;
+  if (i < 2 * C) {
+#pragma unroll 4
+    for (int r = ty; r < rows; r += 32) s += part[(size_t)r * 2 * C + i];
+  }
+  sm[ty][tx] = s;
+  __syncthreads();
+  // a warp per column: lane k joins chain k
+  double v = sm[tx][ty];
+  for (int o = 1; o < 32; o *= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
+  const int j = blockIdx.x * 32 + ty;
+  if (tx == 0 && j < 2 * C) (j < C ? dbeta[j] : dgamma[j - C]) = (float)v;
+}
+
 struct GnPlan {
-  int V, slices, CS, clusters;
+  int V, slices, CS, blocks, rows, stride;
+  int TS, threads, rpc, hold, buffers;  // held form: TS > 0
   size_t smem;
 };
 
+// Channels of a slice as the held form wants them: whole groups, a power of two of 16-byte pieces up to a warp's; false: none
+bool slice_lanes(int C, int cpg, int full, int* least, int* most) {
+  if (C % full) return false;
+  const bool fine = cpg < full;
+  if (fine ? full % cpg != 0 : cpg % full != 0 || ((cpg / full) & (cpg / full - 1)) || cpg / full > 32) return false;
+  *least = *most = fine ? 1 : cpg / full;
+  while (*most < 32 && C % (2 * *most * full) == 0) *most *= 2;
+  return true;
+}
+
+constexpr int kHeldBytes = 92 * 1024;  // of shared memory for two blocks of 256 threads on an SM; one of 512 has twice that
+
+// The held form.  Slices are 128 bytes of a pixel at least, where it has that many: at 64 the backward pass of 1904 images of 16x16x256 took 188 us,
+// at 128 145; at 32 the forward pass of 64 images of 224x224x64 608 us for 260 (other blocks read the rest of a line at other times).  Small images: the smallest
+// team (a warp to 256 threads) that holds a slice in kPer pieces a thread, the slice as wide as that allows.  Larger ones: blocks of 256
+// threads, two on an SM, or one of 512, in clusters that grow until the slice fits, or until there is work for the SMs; what sixteen blocks cannot
+// hold is read twice.
+bool plan_held(int N, int P, int C, int cpg, int full, bool bwd, GnPlan* pl) {
+  int least, most;
+  if (!slice_lanes(C, cpg, full, &least, &most)) return false;
+  const int tensors = bwd ? 2 : 1, kPer = bwd ? 4 : 8;
+  const int wide = most < 8 ? most : 8 > least ? 8 : least;
+  auto fill = [&](int lanes, int TS, int threads, int CS) {
+    pl->V = full;
+    pl->TS = TS;
+    pl->threads = threads;
+    pl->CS = CS;
+    pl->slices = C / (lanes * full);
+    pl->rpc = (P + CS - 1) / CS;
+    const long room = threads == 256 ? kHeldBytes : 2 * kHeldBytes, most_held = room / (threads * 16l * tensors);
+    const long all = ((long)pl->rpc * lanes + TS - 1) / TS;
+    pl->hold = (int)(all < most_held ? all : most_held);
+    const long one = (long)pl->hold * threads * 16 * tensors;
+    pl->buffers = (int)(room / one < 4 ? room / one : 4);
+    const long teams = threads / TS, slots = (long)(threads == 256 ? 296 : 148) / CS * teams;  // teams at a time
+    long per = slots / pl->slices;
+    if (per > N) per = N;
+    if (per < 1) per = 1;
+    while (per * pl->slices % teams) ++per;
+    pl->stride = (int)per;
+    pl->blocks = (int)(per * pl->slices / teams * CS);
+    pl->rows = (int)per * CS;
+    const long fold = bwd ? 2l * full * threads * 4 : 0;
+    pl->smem = (size_t)(pl->buffers * one > fold ? pl->buffers * one : fold);
+  };
+  for (int TS = 32; TS <= 256; TS *= 2) {
+    int lanes = most;
+    while (lanes > wide && ((long)P * lanes > (long)TS * kPer || (long)N * (C / (lanes * full)) * TS < 296 * 256)) lanes /= 2;
+    if ((long)P * lanes > (long)TS * kPer || lanes * full / cpg > 32) continue;
+    if (TS < 256 && (long)N * (C / (lanes * full)) * TS < 148 * 256) continue;  // few images: wider teams
+    fill(lanes, TS, 256, 1);
+    return true;
+  }
+  if (wide * full / cpg > 32) return false;
+  for (int form = 0; form < 3; ++form) {
+    const int threads = form < 2 ? 256 : 512, top = form == 0 ? 8 : kMaxCluster;
+    const long room = threads == 256 ? kHeldBytes : 2 * kHeldBytes, items = (long)N * (C / (wide * full));
+    auto bytes = [&](int cs) { return (((long)(P + cs - 1) / cs * wide + threads - 1) / threads) * threads * 16 * tensors; };
+    int CS = 1;
+    while (CS < top && CS < P && (bytes(CS) > room || (items * CS < 148 && bytes(CS) > 16384))) CS *= 2;
+    if (bytes(CS) > room && form < 2) continue;
+    fill(wide, threads, threads, CS);
+    return true;
+  }
+  return false;
+}
+
 GnPlan plan_gn(int dtype, int N, int P, int C, int groups, bool bwd) {
-  GnPlan pl;
+  GnPlan pl{};
   const int cpg = C / groups;
-  const size_t es = nf_esize(dtype), image = (size_t)P * C * es;
+  const size_t es = nf_esize(dtype);
+  if (plan_held(N, P, C, cpg, 16 / (int)es, bwd, &pl)) return pl;
+  const size_t image = (size_t)P * C * es * (bwd ? 2 : 1);
   // 16 bytes per thread where the slices allow it, else single channels.  A slice is some whole groups: all of them, fewer where C is
-  // above kMaxCs or where one image per (largest portable) cluster would leave most SMs idle, as long as a pixel of it is 64 bytes.
+  // above kMaxCs, where one image per (largest portable) cluster would leave most SMs idle, or where the images in work (two blocks
+  // on each SM) would fill half of L2 -- but not below 64 bytes of a pixel.
   for (pl.V = 16 / (int)es;; pl.V = 1) {
     pl.slices = 0;
     for (int s = 1; s <= groups; ++s) {
       if (groups % s || C / s > kMaxCs || C / s % pl.V) continue;
-      if (pl.slices && ((C / s) * es < 64 || (long)N * s * 8 > 296)) break;
+      if (pl.slices && ((C / s) * es < 64 || ((long)N * pl.slices * 8 >= 296 && image / pl.slices / kMaxCluster <= 200000))) break;
       pl.slices = s;
     }
     if (pl.slices || pl.V == 1) break;
@@ -312,10 +922,12 @@ GnPlan plan_gn(int dtype, int N, int P, int C, int groups, bool bwd) {
   pl.CS = 1;
   while (pl.CS < kMaxCluster && pl.CS < P && (slab / pl.CS > 65536 || (items * pl.CS < 296 && slab / pl.CS > 8192))) pl.CS *= 2;
   if (pl.CS > P) pl.CS = 1;
-  long most = kMaxParts / (pl.CS * pl.slices);
+  long most = kMaxBlocks / (pl.CS * pl.slices);
   if (most < 1) most = 1;
   if (most > N) most = N;
-  pl.clusters = (int)most * pl.slices;
+  pl.blocks = (int)most * pl.slices * pl.CS;
+  pl.stride = (int)most;
+  pl.rows = (int)most * pl.CS;
   const int Cs = C / pl.slices;
   pl.smem = sizeof(float) * ((size_t)2 * pl.V * kNT + 4 * Cs + 2 * (Cs / cpg) + (bwd ? 2 * Cs : 0));
   return pl;
@@ -325,34 +937,97 @@ bool gn_args_ok(int dtype, int N, int P, int C, int groups) {
   return (dtype == NF_F32 || dtype == NF_BF16) && N >= 1 && P >= 1 && C >= 1 && groups >= 1 && C % groups == 0;
 }
 
-template <typename T, int V, bool BWD>
-int launch_gn(const GnArgs& a, const GnPlan& pl) {
+// Clusters of a kernel that are on the GPU at a time: a cluster more than that would only start when the others have done all their images
+template <typename K>
+int resident_clusters(K kernel, int CS, int threads, size_t smem, int* out) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = CS;
+  cfg.blockDim = threads;
+  cfg.dynamicSmemBytes = smem;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = CS;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  NF_CUDA(cudaOccupancyMaxActiveClusters(out, kernel, &cfg));
+  return NF_OK;
+}
+
+template <typename T, int V, int ACT, bool BWD>
+int launch_gn(GnArgs& a, GnPlan& pl) {
   static bool ready[64];
+  static int resident[64][2][2][5];  // [device][FINE][512 threads][log2 CS]; 0: not asked yet
   int dev = 0;
   NF_CUDA(cudaGetDevice(&dev));
   if (dev < 0 || dev >= 64) return NF_EUNSUPPORTED;
-  auto k = group_norm_kernel<T, V, BWD>;
-  if (!ready[dev]) {
-    NF_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024));
+  auto allow = [](auto k, int smem) -> int {
+    NF_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     NF_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    return NF_OK;
+  };
+  auto k = group_norm_kernel<T, V, ACT, BWD>;
+  if (!ready[dev]) {
+    int rc = allow(k, 200 * 1024);
+    if constexpr (V > 1) {
+      if (rc == NF_OK) rc = allow(group_norm_held_kernel<T, V, ACT, BWD, true, 256, false>, kHeldBytes);
+      if (rc == NF_OK) rc = allow(group_norm_held_kernel<T, V, ACT, BWD, false, 256, false>, kHeldBytes);
+      if (rc == NF_OK) rc = allow(group_norm_held_kernel<T, V, ACT, BWD, true, 512, true>, 2 * kHeldBytes);
+      if (rc == NF_OK) rc = allow(group_norm_held_kernel<T, V, ACT, BWD, false, 512, true>, 2 * kHeldBytes);
+    }
+    if (rc != NF_OK) return rc;
     ready[dev] = true;
   }
-  nf_launch_cluster(k, (unsigned)(pl.clusters * pl.CS), kNT, pl.smem, pl.CS, a);
+  if constexpr (V > 1) {
+    if (pl.TS) {
+      const bool fine = a.cpg < V;
+      auto held = fine ? (pl.threads == 512 ? group_norm_held_kernel<T, V, ACT, BWD, true, 512, true> : group_norm_held_kernel<T, V, ACT, BWD, true, 256, false>)
+                       : (pl.threads == 512 ? group_norm_held_kernel<T, V, ACT, BWD, false, 512, true> : group_norm_held_kernel<T, V, ACT, BWD, false, 256, false>);
+      if (pl.CS > 1) {
+        int lg = 0;
+        while (1 << lg < pl.CS) ++lg;
+        int& most = resident[dev][fine][pl.threads == 512][lg];
+        if (!most) {
+          const int rc = resident_clusters(held, pl.CS, pl.threads, pl.threads == 512 ? 2 * kHeldBytes : kHeldBytes, &most);
+          if (rc != NF_OK) return rc;
+        }
+        if (most < 1) return NF_EUNSUPPORTED;
+        if (pl.blocks / pl.CS > most && pl.slices <= most) {
+          a.stride = most / pl.slices;
+          pl.blocks = a.stride * pl.slices * pl.CS;
+          pl.rows = a.stride * pl.CS;
+        }
+      }
+      nf_launch_cluster(held, (unsigned)pl.blocks, pl.threads, pl.smem, pl.CS, a);
+      NF_LAUNCHED();
+      return NF_OK;
+    }
+  }
+  nf_launch_cluster(k, (unsigned)pl.blocks, kNT, pl.smem, pl.CS, a);
   NF_LAUNCHED();
   return NF_OK;
 }
 
+// bf16 has a kernel per activation; fp32 and odd channel counts ask at run time
 template <bool BWD>
-int run_gn(int dtype, const GnArgs& a, const GnPlan& pl) {
-  if (dtype == NF_F32) return pl.V == 4 ? launch_gn<float, 4, BWD>(a, pl) : launch_gn<float, 1, BWD>(a, pl);
-  return pl.V == 8 ? launch_gn<bf16, 8, BWD>(a, pl) : launch_gn<bf16, 1, BWD>(a, pl);
+int run_gn(int dtype, GnArgs& a, GnPlan& pl) {
+  if (dtype == NF_F32) return pl.V == 4 ? launch_gn<float, 4, kAnyAct, BWD>(a, pl) : launch_gn<float, 1, kAnyAct, BWD>(a, pl);
+  if (pl.V == 1) return launch_gn<bf16, 1, kAnyAct, BWD>(a, pl);
+  switch (a.act) {
+    case NF_ACT_NONE: return launch_gn<bf16, 8, NF_ACT_NONE, BWD>(a, pl);
+    case NF_ACT_RELU: return launch_gn<bf16, 8, NF_ACT_RELU, BWD>(a, pl);
+    case NF_ACT_SILU: return launch_gn<bf16, 8, NF_ACT_SILU, BWD>(a, pl);
+    default: return launch_gn<bf16, 8, NF_ACT_GELU, BWD>(a, pl);
+  }
 }
 
-void fill_gn(GnArgs& a, const GnPlan& pl, int N, int P, int C, int groups, int act) {
+int fill_gn(GnArgs& a, const GnPlan& pl, int N, int P, int C, int groups, int act) {
   a.N = N; a.P = P; a.C = C; a.G = groups; a.cpg = C / groups;
   a.slices = pl.slices; a.Cs = C / pl.slices; a.vpr = a.Cs / pl.V;
-  a.CS = pl.CS; a.stride = pl.clusters / pl.slices;
+  a.CS = pl.CS; a.stride = pl.stride; a.TS = pl.TS;
+  a.rpc = pl.rpc; a.hold = pl.hold; a.buffers = pl.buffers;
   a.act = act;
+  return nf_tc_op_status_ptr(&a.status);
 }
 
 }  // namespace
@@ -364,17 +1039,16 @@ extern "C" int nf_group_norm_forward(int dtype, const void* x, const float* gamm
   if (C / groups > kMaxCs) return NF_EUNSUPPORTED;
   const size_t bytes = (size_t)N * P * C * nf_esize(dtype);
   if (nf_overlap(x, bytes, y, bytes)) return NF_EINVAL;
-  const GnPlan pl = plan_gn(dtype, N, P, C, groups, false);
+  GnPlan pl = plan_gn(dtype, N, P, C, groups, false);
   GnArgs a{};
-  fill_gn(a, pl, N, P, C, groups, act);
+  if (fill_gn(a, pl, N, P, C, groups, act) != NF_OK) return NF_ECUDA;
   a.x = x; a.gamma = gamma; a.beta = beta; a.out = y; a.mean = mean; a.rstd = rstd; a.eps = eps;
   return run_gn<false>(dtype, a, pl);
 }
 
 extern "C" size_t nf_group_norm_scratch_bytes(int dtype, int N, int P, int C, int groups) {
   if (!gn_args_ok(dtype, N, P, C, groups) || C / groups > kMaxCs) return 0;
-  const GnPlan pl = plan_gn(dtype, N, P, C, groups, true);
-  return (size_t)pl.clusters / pl.slices * pl.CS * 2 * C * sizeof(float);
+  return (size_t)plan_gn(dtype, N, P, C, groups, true).rows * 2 * C * sizeof(float);
 }
 
 extern "C" int nf_group_norm_backward(int dtype, const void* x, const void* dy, const float* gamma, const float* beta, const float* mean,
@@ -387,17 +1061,17 @@ extern "C" int nf_group_norm_backward(int dtype, const void* x, const void* dy, 
        (uintptr_t)dx | (uintptr_t)dgamma | (uintptr_t)dbeta) & 15)
     return NF_EALIGN;
   if (C / groups > kMaxCs) return NF_EUNSUPPORTED;
-  const size_t bytes = (size_t)N * P * C * nf_esize(dtype), need = nf_group_norm_scratch_bytes(dtype, N, P, C, groups);
-  if (scratch_bytes < need) return NF_ENOWS;
+  const size_t bytes = (size_t)N * P * C * nf_esize(dtype);
+  GnPlan pl = plan_gn(dtype, N, P, C, groups, true);
+  if (scratch_bytes < (size_t)pl.rows * 2 * C * sizeof(float)) return NF_ENOWS;
   if (nf_overlap(x, bytes, dx, bytes) || nf_overlap(dy, bytes, dx, bytes)) return NF_EINVAL;
-  const GnPlan pl = plan_gn(dtype, N, P, C, groups, true);
   GnArgs a{};
-  fill_gn(a, pl, N, P, C, groups, act);
+  if (fill_gn(a, pl, N, P, C, groups, act) != NF_OK) return NF_ECUDA;
   a.x = x; a.dy = dy; a.gamma = gamma; a.beta = beta; a.out = dx; a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);
   a.part = (float*)scratch;
   const int rc = run_gn<true>(dtype, a, pl);
   if (rc != NF_OK) return rc;
-  nf_launch(group_norm_param_kernel, (unsigned)((2 * C + 31) / 32), 256, 0, (const float*)scratch, a.stride * pl.CS, C, dgamma, dbeta);
+  nf_launch(group_norm_param_kernel, (unsigned)((2 * C + 31) / 32), 1024, 0, (const float*)scratch, pl.rows, C, dgamma, dbeta);
   NF_LAUNCHED();
   return NF_OK;
 }

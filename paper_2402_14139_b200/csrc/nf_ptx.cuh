@@ -181,6 +181,14 @@ __device__ __forceinline__ void mbar_arrive_rank(uint64_t* bar, uint32_t rank) {
                "r"(rank)
                : "memory");
 }
+// Two floats to this place in block `rank`, counted (8 bytes) by the barrier at this place there
+__device__ __forceinline__ void st_async_f2(const void* dst, float x, float y, uint64_t* bar, uint32_t rank) {
+  asm volatile(
+      "{\n.reg .b32 rd, rb;\nmapa.shared::cluster.u32 rd, %0, %4;\nmapa.shared::cluster.u32 rb, %3, %4;\n"
+      "st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [rd], {%1, %2}, [rb];\n}" ::"r"(smem_u32(dst)),
+      "f"(x), "f"(y), "r"(smem_u32(bar)), "r"(rank)
+      : "memory");
+}
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
