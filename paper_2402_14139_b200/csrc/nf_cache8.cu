@@ -15,15 +15,46 @@ namespace {
 constexpr uint32_t kFloorBits = 27u << 23;  // 2^-100 as a float: (127 - 100) << 23
 template <int F> constexpr float kTop = F == NF_Q_INT8 ? 127.f : 448.f;
 
+// Codes of x * (top / a), whose magnitude is at most the top, or one rounding above it.  int8: adding 1.5 * 2^23 rounds to an integer,
+// ties to even, and leaves it in the low byte.
 template <int F>
-__device__ __forceinline__ uint32_t code_of(float q) {  // the code of x * (top / a)
-  if constexpr (F == NF_Q_INT8) return (uint32_t)(__float2int_rn(fminf(fmaxf(q, -127.f), 127.f)) & 255);
+__device__ __forceinline__ uint32_t code_of(float q) {
+  if constexpr (F == NF_Q_INT8) return __float_as_uint(__fadd_rn(q, 12582912.f)) & 255u;  // not fused with the product before it
   return (uint32_t)__nv_cvt_float_to_fp8(q, __NV_SATFINITE, __NV_E4M3);
+}
+template <int F>
+__device__ __forceinline__ uint32_t codes4(f32x2 q01, f32x2 q23) {
+  float a, b, c, d;
+  if constexpr (F == NF_Q_INT8) {
+    const f32x2 magic = nf_pack2(12582912.f, 12582912.f);
+    nf_unpack2(nf_add_each(q01, magic), a, b);
+    nf_unpack2(nf_add_each(q23, magic), c, d);
+    return __byte_perm(__byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0040), __byte_perm(__float_as_uint(c), __float_as_uint(d), 0x0040), 0x5410);
+  }
+  nf_unpack2(q01, a, b);
+  nf_unpack2(q23, c, d);
+  return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3) |
+         (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3) << 16;
 }
 template <int F>
 __device__ __forceinline__ float value_of(uint32_t code) {
   if constexpr (F == NF_Q_INT8) return (float)(int8_t)code;
   return __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)code, __NV_E4M3)));
+}
+// The values of the four codes in w.  int8: a code offset by 128 is the low byte of a float whose unit is 1.
+template <int F>
+__device__ __forceinline__ void values4(uint32_t w, f32x2& v01, f32x2& v23) {
+  if constexpr (F == NF_Q_INT8) {
+    const uint32_t u = w ^ 0x80808080u;
+    const f32x2 back = nf_pack2(-8388736.f, -8388736.f);  // 2^23 + 128
+    v01 = nf_add2(nf_pack2(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7540)), __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7541))), back);
+    v23 = nf_add2(nf_pack2(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7542)), __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7543))), back);
+  } else {
+    const float2 a = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w & 0xffffu), __NV_E4M3)));
+    const float2 b = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> 16), __NV_E4M3)));
+    v01 = nf_pack2(a.x, a.y);
+    v23 = nf_pack2(b.x, b.y);
+  }
 }
 // Scale and reciprocal from the largest magnitude's bits.  A group that holds a NaN or an infinity (whose bits are above those of every
 // finite number) gets a NaN for a scale, so that all of it reads back as NaN, and raises the flag.
@@ -52,13 +83,29 @@ __global__ void __launch_bounds__(256) quantize_vec_kernel(const T* __restrict__
   const uint32_t gi = (uint32_t)(g - row * groups), k = gi * LG + (uint32_t)(slot % LG);
   const bool on = k < per_row && row * per_row < pieces;
   const size_t e = row * per_row + k;
-  float v[16];
+  f32x2 v[8];
   uint32_t top = 0;
   if (on) {
-    ld8(x + e * 16, *reinterpret_cast<float(*)[8]>(v));
-    ld8(x + e * 16 + 8, *reinterpret_cast<float(*)[8]>(v + 8));
+    if constexpr (sizeof(T) == 2) {  // magnitudes of bf16 pairs compared as they lie
+      const uint4 a = __ldcs(reinterpret_cast<const uint4*>(x + e * 16)), b = __ldcs(reinterpret_cast<const uint4*>(x + e * 16 + 8));
+      const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+      uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+      for (int i = 0; i < 8; ++i) {
+        m = __vmaxu2(m, w[i] & 0x7fff7fffu);
+        v[i] = nf_pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+      }
+      top = max(m & 0xffff0000u, m << 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float4 a = __ldcs(reinterpret_cast<const float4*>(x + e * 16 + 4 * i));
+        v[2 * i] = nf_pack2(a.x, a.y);
+        v[2 * i + 1] = nf_pack2(a.z, a.w);
+        top = max(top, max(max(__float_as_uint(a.x) & 0x7fffffffu, __float_as_uint(a.y) & 0x7fffffffu),
+                           max(__float_as_uint(a.z) & 0x7fffffffu, __float_as_uint(a.w) & 0x7fffffffu)));
+      }
+    }
   }
 #pragma unroll
   for (int o = 1; o < LG; o *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
@@ -66,72 +113,98 @@ __global__ void __launch_bounds__(256) quantize_vec_kernel(const T* __restrict__
   float r;
   const float s = scale_of<F>(top, &r, status);
   uint32_t w[4];
+  const f32x2 rr = nf_pack2(r, r);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    w[i] = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) w[i] |= code_of<F>(v[4 * i + j] * r) << (8 * j);
-  }
+  for (int i = 0; i < 4; ++i) w[i] = codes4<F>(nf_mul2(v[2 * i], rr), nf_mul2(v[2 * i + 1], rr));
   codes[e] = make_uint4(w[0], w[1], w[2], w[3]);
   if (slot % LG == 0) scales[g] = s;
 }
 
-// Any row length: a warp per group
-template <int F, typename T>
-__global__ void __launch_bounds__(256) quantize_any_kernel(const T* __restrict__ x, size_t total_groups, size_t row_elems, uint32_t groups,
-                                                           int group, uint8_t* __restrict__ codes, float* __restrict__ scales,
-                                                           int32_t* status) {
+// Any row length: a warp takes kWarpGroups neighbouring groups of a row, a lane every 32nd element; no piece is aligned, so loads and stores
+// are single elements, 32 neighbours at a time.
+constexpr int kWarpGroups = 4;
+
+template <int F, typename T, int Q>  // Q = group / 32
+__global__ void __launch_bounds__(256) quantize_any_kernel(const T* __restrict__ x, uint32_t row_elems, uint32_t groups, uint32_t chunks,
+                                                           uint8_t* __restrict__ codes, float* __restrict__ scales, int32_t* status) {
   nf_pdl_begin();
   const int lane = threadIdx.x & 31;
-  const size_t g = (size_t)blockIdx.x * 8 + threadIdx.x / 32;
-  if (g >= total_groups) return;
-  const size_t row = g / groups, first = (g - row * groups) * group;
-  const int len = (int)(row_elems - first < (size_t)group ? row_elems - first : (size_t)group);
-  const size_t base = row * row_elems + first;
-  float v[4];
-  uint32_t top = 0;
+  const uint32_t row = blockIdx.x / chunks, g0 = ((blockIdx.x - row * chunks) * 8 + threadIdx.x / 32) * kWarpGroups;
+  const T* from = x + (size_t)row * row_elems;
+  uint8_t* to = codes + (size_t)row * row_elems;
+  float v[kWarpGroups][Q];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[i] = lane + 32 * i < len ? ldf(x, base + lane + 32 * i) : 0.f;
-    top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+  for (int j = 0; j < kWarpGroups; ++j)
+#pragma unroll
+    for (int i = 0; i < Q; ++i) {
+      const uint32_t k = (g0 + j) * (32 * Q) + 32 * i + lane;
+      v[j][i] = g0 + j < groups && k < row_elems ? ldf(from, k) : 0.f;
+    }
+#pragma unroll
+  for (int j = 0; j < kWarpGroups; ++j) {
+    if (g0 + j >= groups) return;  // the whole warp
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < Q; ++i) top = max(top, __float_as_uint(v[j][i]) & 0x7fffffffu);
+    top = __reduce_max_sync(0xffffffffu, top);
+    float r;
+    const float s = scale_of<F>(top, &r, status);
+#pragma unroll
+    for (int i = 0; i < Q; ++i) {
+      const uint32_t k = (g0 + j) * (32 * Q) + 32 * i + lane;
+      if (k < row_elems) to[k] = (uint8_t)code_of<F>(__fmul_rn(v[j][i], r));
+    }
+    if (lane == 0) scales[(size_t)row * groups + g0 + j] = s;
   }
-#pragma unroll
-  for (int o = 1; o < 32; o *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-  float r;
-  const float s = scale_of<F>(top, &r, status);
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (lane + 32 * i < len) codes[base + lane + 32 * i] = (uint8_t)code_of<F>(v[i] * r);
-  if (lane == 0) scales[g] = s;
 }
 
-// One piece of 16 elements per thread; out of range indices as in nf_cache_gather
+// Row r of the output from row idx[r] of the cache; indices out of range as in nf_cache_gather.  A block takes kGatherSpan elements of one
+// row: pieces of 8 codes (one 16-byte store of bf16), or, where rows are not made of such pieces, single elements.
+constexpr int kGatherSpan = 8192;
+
 template <int F, typename T>
-__global__ void __launch_bounds__(256) gather_vec_kernel(const uint4* __restrict__ codes, const float* __restrict__ scales,
-                                                         const int32_t* __restrict__ labels, int cache_rows,
-                                                         const int32_t* __restrict__ idx, uint32_t per_row, uint32_t groups, int lg_log,
-                                                         size_t total, T* __restrict__ out, int32_t* __restrict__ out_labels, int32_t* status) {
+__global__ void __launch_bounds__(256) gather_vec_kernel(const uint2* __restrict__ codes, const float* __restrict__ scales,
+                                                         const int32_t* __restrict__ labels, int cache_rows, const int32_t* __restrict__ idx,
+                                                         uint32_t per_row, uint32_t groups, int lg_log, uint32_t chunks, T* __restrict__ out,
+                                                         int32_t* __restrict__ out_labels, int32_t* status) {
   nf_pdl_begin();
-  const size_t e = (size_t)blockIdx.x * 256 + threadIdx.x;
-  if (e >= total) return;
-  const size_t r = e / per_row;
-  const uint32_t k = (uint32_t)(e - r * per_row);
+  const uint32_t r = blockIdx.x / chunks, chunk = blockIdx.x - r * chunks;
   const int32_t src = idx[r];
   const bool ok = src >= 0 && src < cache_rows;
-  float v[16];
-  if (ok) {
-    const uint4 u = codes[(size_t)src * per_row + k];
-    const float s = scales[(size_t)src * groups + (k >> lg_log)];
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+  const uint2* from = codes + (size_t)(ok ? src : 0) * per_row;
+  const float* sc = scales + (size_t)(ok ? src : 0) * groups;
+  T* to = out + (size_t)r * per_row * 8;
+  constexpr int kTurns = kGatherSpan / 8 / 256;
+  const uint32_t k0 = chunk * (kGatherSpan / 8) + threadIdx.x;
+  uint2 u[kTurns];
+  float s[kTurns];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = value_of<F>((w[i / 4] >> (8 * (i % 4))) & 255u) * s;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = 0.f;
+  for (int j = 0; j < kTurns; ++j) {
+    const uint32_t k = k0 + 256 * j;
+    if (k < per_row && ok) {
+      u[j] = __ldcs(from + k);
+      s[j] = sc[k >> lg_log];
+    }
   }
-  st8(out + e * 16, *reinterpret_cast<float(*)[8]>(v));
-  st8(out + e * 16 + 8, *reinterpret_cast<float(*)[8]>(v + 8));
-  if (k == 0) {
+#pragma unroll
+  for (int j = 0; j < kTurns; ++j) {
+    const uint32_t k = k0 + 256 * j;
+    if (k >= per_row) break;
+    float f[8];
+    if (ok) {
+      f32x2 v[4];
+      const f32x2 ss = nf_pack2(s[j], s[j]);
+      values4<F>(u[j].x, v[0], v[1]);
+      values4<F>(u[j].y, v[2], v[3]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) nf_unpack2(nf_mul2(v[i], ss), f[2 * i], f[2 * i + 1]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] = 0.f;
+    }
+    st8(to + (size_t)k * 8, f);
+  }
+  if (chunk == 0 && threadIdx.x == 0) {
     if (out_labels) out_labels[r] = ok ? labels[src] : -1;
     if (!ok) atomicOr(status, NF_EINDEX);
   }
@@ -139,17 +212,20 @@ __global__ void __launch_bounds__(256) gather_vec_kernel(const uint4* __restrict
 
 template <int F, typename T>
 __global__ void __launch_bounds__(256) gather_any_kernel(const uint8_t* __restrict__ codes, const float* __restrict__ scales,
-                                                         const int32_t* __restrict__ labels, int cache_rows,
-                                                         const int32_t* __restrict__ idx, size_t row_elems, size_t groups, int group,
-                                                         size_t total, T* __restrict__ out, int32_t* __restrict__ out_labels, int32_t* status) {
+                                                         const int32_t* __restrict__ labels, int cache_rows, const int32_t* __restrict__ idx,
+                                                         uint32_t row_elems, uint32_t groups, int group_log, uint32_t chunks, T* __restrict__ out,
+                                                         int32_t* __restrict__ out_labels, int32_t* status) {
   nf_pdl_begin();
-  const size_t e = (size_t)blockIdx.x * 256 + threadIdx.x;
-  if (e >= total) return;
-  const size_t r = e / row_elems, k = e - r * row_elems;
+  const uint32_t r = blockIdx.x / chunks, chunk = blockIdx.x - r * chunks;
   const int32_t src = idx[r];
   const bool ok = src >= 0 && src < cache_rows;
-  stf(out, e, ok ? value_of<F>(codes[(size_t)src * row_elems + k]) * scales[(size_t)src * groups + k / group] : 0.f);
-  if (k == 0) {
+  const uint8_t* from = codes + (size_t)(ok ? src : 0) * row_elems;
+  const float* sc = scales + (size_t)(ok ? src : 0) * groups;
+  T* to = out + (size_t)r * row_elems;
+  const uint32_t end = min(row_elems, (chunk + 1) * kGatherSpan);
+#pragma unroll 8
+  for (uint32_t k = chunk * kGatherSpan + threadIdx.x; k < end; k += 256) stf(to, k, ok ? value_of<F>(from[k]) * sc[k >> group_log] : 0.f);
+  if (chunk == 0 && threadIdx.x == 0) {
     if (out_labels) out_labels[r] = ok ? labels[src] : -1;
     if (!ok) atomicOr(status, NF_EINDEX);
   }
@@ -170,9 +246,10 @@ int quantize(const T* x, int rows, long long E, int group, uint8_t* codes, float
     auto k = LG == 2 ? quantize_vec_kernel<F, T, 2> : LG == 4 ? quantize_vec_kernel<F, T, 4> : quantize_vec_kernel<F, T, 8>;
     nf_launch(k, (unsigned)blocks, 256, 0, x, (size_t)rows * (E / 16), (uint32_t)(E / 16), (uint32_t)groups, (uint4*)codes, scales, st);
   } else {
-    const size_t blocks = (total + 7) / 8;
+    const size_t chunks = (groups + 8 * kWarpGroups - 1) / (8 * kWarpGroups), blocks = chunks * rows;
     if (blocks > 0x7fffffffull) return NF_EUNSUPPORTED;
-    nf_launch(quantize_any_kernel<F, T>, (unsigned)blocks, 256, 0, x, total, (size_t)E, (uint32_t)groups, group, codes, scales, st);
+    auto k = group == 32 ? quantize_any_kernel<F, T, 1> : group == 64 ? quantize_any_kernel<F, T, 2> : quantize_any_kernel<F, T, 4>;
+    nf_launch(k, (unsigned)blocks, 256, 0, x, (uint32_t)E, (uint32_t)groups, (uint32_t)chunks, codes, scales, st);
   }
   NF_LAUNCHED();
   return NF_OK;
@@ -181,16 +258,15 @@ int quantize(const T* x, int rows, long long E, int group, uint8_t* codes, float
 template <int F, typename T>
 int gather(const uint8_t* codes, const float* scales, const int32_t* labels, int cache_rows, const int32_t* idx, int count, long long E,
            int group, T* out, int32_t* out_labels, int32_t* st) {
-  const size_t groups = (size_t)((E + group - 1) / group);
-  const bool vec = E % 16 == 0;
-  const size_t total = (size_t)count * (vec ? E / 16 : E), blocks = (total + 255) / 256;
+  const size_t groups = (size_t)((E + group - 1) / group), chunks = (size_t)(E + kGatherSpan - 1) / kGatherSpan, blocks = chunks * count;
+  const int lg = group == 32 ? 5 : group == 64 ? 6 : 7;
   if (blocks > 0x7fffffffull) return NF_EUNSUPPORTED;
-  if (vec)
-    nf_launch(gather_vec_kernel<F, T>, (unsigned)blocks, 256, 0, (const uint4*)codes, scales, labels, cache_rows, idx, (uint32_t)(E / 16),
-              (uint32_t)groups, group == 32 ? 1 : group == 64 ? 2 : 3, total, out, out_labels, st);
+  if (E % 8 == 0)
+    nf_launch(gather_vec_kernel<F, T>, (unsigned)blocks, 256, 0, (const uint2*)codes, scales, labels, cache_rows, idx, (uint32_t)(E / 8),
+              (uint32_t)groups, lg - 3, (uint32_t)chunks, out, out_labels, st);
   else
-    nf_launch(gather_any_kernel<F, T>, (unsigned)blocks, 256, 0, codes, scales, labels, cache_rows, idx, (size_t)E, groups, group, total, out,
-              out_labels, st);
+    nf_launch(gather_any_kernel<F, T>, (unsigned)blocks, 256, 0, codes, scales, labels, cache_rows, idx, (uint32_t)E, (uint32_t)groups, lg,
+              (uint32_t)chunks, out, out_labels, st);
   NF_LAUNCHED();
   return NF_OK;
 }

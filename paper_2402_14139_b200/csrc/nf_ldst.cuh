@@ -60,8 +60,16 @@ __device__ __forceinline__ f32x2 nf_add2(f32x2 a, f32x2 b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
+// The assembler joins a packed product and a packed sum of it to one multiply-add, whatever rounding they name: where the product has to be
+// rounded by itself, the sum is taken by nf_add_each.
 __device__ __forceinline__ f32x2 nf_mul2(f32x2 a, f32x2 b) {
   f32x2 r;
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
+}
+__device__ __forceinline__ f32x2 nf_add_each(f32x2 a, f32x2 b) {
+  float a0, a1, b0, b1;
+  nf_unpack2(a, a0, a1);
+  nf_unpack2(b, b0, b1);
+  return nf_pack2(__fadd_rn(a0, b0), __fadd_rn(a1, b1));
 }

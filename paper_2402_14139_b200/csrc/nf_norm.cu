@@ -10,8 +10,8 @@
 //  - any other shape: a cluster of blocks reads its slice twice, the second time from L2.
 // Parameter gradients gather in registers or shared memory over all images of a team or block, then in one row of partials each.
 //
-// Sums: a thread adds in fp32 what it sees of its channels, in the forward pass after subtracting a value of the group or channel, so that a mean far from zero costs no digits; ranges of pixels are joined by their means and squared deviations.  xh and z
-// are formed by separately rounded operations in this order in both directions, so that the gradient's ReLU mask is the forward's.
+// Sums: a thread adds in fp32 what it sees of its channels, in the forward pass after subtracting a value of the group or channel, so that a mean far from zero costs no digits; ranges of pixels are joined by their means and squared deviations.  For ReLU
+// xh and z are formed by separately rounded operations in this order in both directions, so that the gradient's mask is the forward's.
 #include <cooperative_groups.h>
 
 #include <cuda.h>
@@ -150,7 +150,12 @@ struct Chan {
   }
   __device__ __forceinline__ f32x2 scale(int i) const { return rs[ONE ? 0 : i]; }
   __device__ __forceinline__ f32x2 xh(f32x2 x, int i) const { return nf_mul2(nf_add2(x, nmu[ONE ? 0 : i]), rs[ONE ? 0 : i]); }
-  __device__ __forceinline__ f32x2 z(f32x2 xh, int i) const { return nf_add2(nf_mul2(xh, ga[i]), be[i]); }
+  // ReLU, whose gradient is a decision on the sign: product and sum rounded one by one in both directions; else in one
+  template <int ACT>
+  __device__ __forceinline__ f32x2 z(f32x2 xh, int i) const {
+    if constexpr (ACT == NF_ACT_RELU || ACT == kAnyAct) return nf_add_each(nf_mul2(xh, ga[i]), be[i]);
+    return nf_fma2(xh, ga[i], be[i]);
+  }
 };
 
 // ---------------------------------------------------------------- large images
@@ -209,7 +214,7 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_kernel(const GnArgs a) {
           for (int i = 0; i < NP; ++i) {
             if constexpr (BWD) {
               const f32x2 xh = ch.xh(v.pair(i), i);
-              const f32x2 dz = grad2<T, ACT>(ACT == NF_ACT_NONE ? xh : ch.z(xh, i), g.pair(i), a.act);
+              const f32x2 dz = grad2<T, ACT>(ACT == NF_ACT_NONE ? xh : ch.template z<ACT>(xh, i), g.pair(i), a.act);
               s[i] = nf_add2(s[i], dz);
               q[i] = nf_fma2(dz, xh, q[i]);
             } else {
@@ -340,10 +345,10 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_kernel(const GnArgs a) {
         for (int i = 0; i < NP; ++i) {
           const f32x2 xh = ch.xh(v.pair(i), i);
           if constexpr (BWD) {
-            const f32x2 dz = grad2<T, ACT>(ACT == NF_ACT_NONE ? xh : ch.z(xh, i), g.pair(i), a.act);
+            const f32x2 dz = grad2<T, ACT>(ACT == NF_ACT_NONE ? xh : ch.template z<ACT>(xh, i), g.pair(i), a.act);
             o[i] = nf_mul2(ch.scale(i), nf_fma2(xh, m2[i], nf_fma2(ch.ga[i], dz, m1[i])));
           } else {
-            o[i] = act2<T, ACT>(ch.z(xh, i), a.act);
+            o[i] = act2<T, ACT>(ch.template z<ACT>(xh, i), a.act);
           }
         }
         store<T, V>(to, o);
@@ -502,7 +507,7 @@ __global__ void __launch_bounds__(NT, 512 / NT) group_norm_held_kernel(const GnA
       for (int i = 0; i < NP; ++i) {
         if constexpr (BWD) {
           const f32x2 xh = ch.xh(v.pair(i), i);
-          const f32x2 dz = grad2<T, ACT>(ACT == NF_ACT_NONE ? xh : ch.z(xh, i), g.pair(i), a.act);
+          const f32x2 dz = grad2<T, ACT>(ACT == NF_ACT_NONE ? xh : ch.template z<ACT>(xh, i), g.pair(i), a.act);
           s[i] = nf_add2(s[i], dz);
           q[i] = nf_fma2(dz, xh, q[i]);
         } else {
@@ -707,10 +712,10 @@ __global__ void __launch_bounds__(NT, 512 / NT) group_norm_held_kernel(const GnA
       for (int i = 0; i < NP; ++i) {
         const f32x2 xh = ch.xh(v.pair(i), i);
         if constexpr (BWD) {
-          const f32x2 dz = grad2<T, ACT>(ACT == NF_ACT_NONE ? xh : ch.z(xh, i), g.pair(i), a.act);
+          const f32x2 dz = grad2<T, ACT>(ACT == NF_ACT_NONE ? xh : ch.template z<ACT>(xh, i), g.pair(i), a.act);
           o[i] = nf_mul2(ch.scale(i), nf_fma2(xh, m2[FINE ? i : 0], nf_fma2(ch.ga[i], dz, m1[FINE ? i : 0])));
         } else {
-          o[i] = act2<T, ACT>(ch.z(xh, i), a.act);
+          o[i] = act2<T, ACT>(ch.template z<ACT>(xh, i), a.act);
         }
       }
       store<T, V>(to, o);
