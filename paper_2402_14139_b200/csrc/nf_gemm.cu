@@ -9,7 +9,8 @@
 // fp32 results: the tensor core cuts low bits off its running sum at every instruction, always towards zero (about 2^-25 of it here), so
 // a sum over thousands of products would lose the digits that fp32 has.  Accumulators then change every `seg` steps of 64 and
 // the warps add them up in registers.  fp32 operands come as three bf16 parts, x = h + m + l exactly, and the six products
-// mm, hl, lh, hm, mh, hh; what is left out is below 2^-24 of |x| |w|.
+// l h, h l, m m, h m, m h, h h; what is left out is below 2^-24 of |x| |w|.  The three parts of a step of 64 lie in three stages side by side,
+// so that each is brought in once for all its products.
 #include <cuda.h>
 
 #include "nf_act.cuh"
@@ -21,11 +22,14 @@ namespace {
 
 constexpr int kGemmThreads = 320;  // warp 0: TMA, warp 1: products, warps 2-9: epilogue
 constexpr int kBox = 64;           // r per operand tile: 128 bytes of bf16
-constexpr int kStaging = 8 * 2 * 4096;  // two tiles of 32 rows x 128 bytes per epilogue warp
+// Tiles of 32 rows x 128 bytes per epilogue warp on their way out: two, or one where sums are long (fp32 results) and a sixth operand stage
+// is worth more: the parts of the next step of 64 are then all on their way while this one's are multiplied
+template <typename T> constexpr int kTiles = sizeof(T) == 4 ? 1 : 2;
+template <typename T> constexpr int kStaging = 8 * kTiles<T> * 4096;
 
 struct GemmParams {
-  int P, Q, kblocks;           // steps of 64 products, all pairs of parts counted
-  int tiles_p, tiles_q, splits, pairs, seg;
+  int P, Q, kblocks;           // operand tiles along r: 64 products each, times the parts
+  int tiles_p, tiles_q, splits, planes, seg;
   int a_along_r, b_along_r;
   int tma_out;                 // rows of C are multiples of 16 bytes: TMA stores them
   Epilogue e;
@@ -113,7 +117,22 @@ __device__ __forceinline__ void tile_to_rows(uint32_t tile, T* dst, int row0, in
     }
 }
 
-// One warp's way out: 32 rows x CH columns at a time.  `turn` counts the tiles of this warp: two staging tiles in turn.
+// One branch per activation, not one per value: with the branch inside the loop the 1x1 product of 200704 x 256 x 256 took 136 us for XX
+template <typename T, int CH>
+__device__ __forceinline__ void activate(float (&v)[CH], int act) {
+  if (act == NF_ACT_RELU) {
+#pragma unroll
+    for (int j = 0; j < CH; ++j) v[j] = nf_act_value<T>(v[j], NF_ACT_RELU);
+  } else if (act == NF_ACT_SILU) {
+#pragma unroll
+    for (int j = 0; j < CH; ++j) v[j] = nf_act_value<T>(v[j], NF_ACT_SILU);
+  } else if (act == NF_ACT_GELU) {
+#pragma unroll
+    for (int j = 0; j < CH; ++j) v[j] = nf_act_value<T>(v[j], NF_ACT_GELU);
+  }
+}
+
+// One warp's way out: 32 rows x CH columns at a time.  `turn` counts the tiles of this warp, which take its staging tiles in turn.
 template <typename T>
 struct WayOut {
   static constexpr int CH = 128 / sizeof(T);
@@ -138,7 +157,7 @@ struct WayOut {
   __device__ __forceinline__ void put(const GemmParams& p, const CUtensorMap* tc, const CUtensorMap* tp, const CUtensorMap* tr, int row0, int col0, int plane,
                                       int next_col, float (&v)[CH]) {
     constexpr int n = Pack<T>::n;
-    const uint32_t b = turn & 1;
+    const uint32_t b = turn & (kTiles<T> - 1);
     ++turn;
     if (row0 >= p.P || col0 >= p.Q) return;  // the whole warp
     const bool whole = p.splits == 1;
@@ -159,7 +178,7 @@ struct WayOut {
     }
     if (whole && p.e.residual) {
       if (p.tma_out) {
-        fetch(p, tr, b ^ 1, row0, next_col);
+        if constexpr (kTiles<T> == 2) fetch(p, tr, b ^ 1, row0, next_col);
         ptx::mbar_wait(&rbar[b], (rphase >> b) & 1, abort_flag);  // sets the abort flag itself when it gives up
         rphase ^= 1u << b;
       } else {
@@ -168,8 +187,9 @@ struct WayOut {
       }
 #pragma unroll
       for (int i = 0; i < CH / n; ++i) Pack<T>::add(ptx::lds128(row + ((i ^ (lane & 7)) << 4)), v + i * n);
-    } else if (p.tma_out && lane == 0) {
-      ptx::tma_store_wait_read_but_one();  // what was stored from this tile the turn before last has been read
+    } else if (p.tma_out && lane == 0) {  // what was stored from this tile before has been read
+      if constexpr (kTiles<T> == 2) ptx::tma_store_wait_read_but_one();
+      else ptx::tma_store_wait_read();
     }
     __syncwarp();
     if (whole && p.e.pre) {
@@ -179,13 +199,11 @@ struct WayOut {
       if (p.tma_out && lane == 0) ptx::tma_store_wait_read();
       __syncwarp();
     }
-    if (whole && p.e.act != NF_ACT_NONE) {
-#pragma unroll
-      for (int j = 0; j < CH; ++j) v[j] = nf_act_value<T>(v[j], p.e.act);
-    }
+    if (whole) activate<T, CH>(v, p.e.act);
 #pragma unroll
     for (int i = 0; i < CH / n; ++i) ptx::sts128(row + ((i ^ (lane & 7)) << 4), Pack<T>::pack(v + i * n));
     send(p, tc, reinterpret_cast<T*>(p.e.out) + (size_t)plane * p.P * p.Q, b, row0, col0, plane);
+    if constexpr (kTiles<T> == 1) fetch(p, tr, b, row0, next_col);  // waits for the store just sent to have been read
   }
   __device__ __forceinline__ void send(const GemmParams& p, const CUtensorMap* m, T* dst, uint32_t b, int row0, int col0, int plane) {
     if (p.tma_out) {
@@ -203,20 +221,20 @@ struct WayOut {
   }
 };
 
-template <int CG, int BN> constexpr int kGemmStages = (227 * 1024 - 1024 - 512 - kStaging) / (128 * 128 + BN / CG * 128);
-template <int CG, int BN> constexpr int kGemmSmem = 1024 + kGemmStages<CG, BN> * (128 * 128 + BN / CG * 128) + kStaging + 512;
+template <int CG, int BN, typename T> constexpr int kGemmStages = (227 * 1024 - 1024 - 512 - kStaging<T>) / (128 * 128 + BN / CG * 128);
+template <int CG, int BN, typename T> constexpr int kGemmSmem = 1024 + kGemmStages<CG, BN, T> * (128 * 128 + BN / CG * 128) + kStaging<T> + 512;
 
 template <int CG, int BN, typename T>
 __global__ void __launch_bounds__(kGemmThreads, 1)
 gemm_tc_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const __grid_constant__ CUtensorMap tm_c,
                const __grid_constant__ CUtensorMap tm_r, const __grid_constant__ CUtensorMap tm_p, const __grid_constant__ GemmParams p) {
   constexpr bool kSegments = sizeof(T) == 4;
-  constexpr int kStages = kGemmStages<CG, BN>, kA = 128 * 128, kB = BN / CG * 128, kStage = kA + kB;
+  constexpr int kStages = kGemmStages<CG, BN, T>, kA = 128 * 128, kB = BN / CG * 128, kStage = kA + kB;
   constexpr uint32_t kCols = 2 * BN;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* staging = smem + kStages * kStage;
-  uint64_t* full = reinterpret_cast<uint64_t*>(staging + kStaging);
+  uint64_t* full = reinterpret_cast<uint64_t*>(staging + kStaging<T>);
   uint64_t* empty = full + kStages;
   uint64_t* tfull = empty + kStages;
   uint64_t* tempty = tfull + 2;
@@ -227,10 +245,10 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = CG == 2 ? ptx::cluster_rank() : 0;
   const int first = blockIdx.x / CG, step = gridDim.x / CG, units = p.tiles_p * p.tiles_q * p.splits;
-  auto k_range = [&](int sp, int& k0, int& k1) {  // whole groups of pairs
-    const int groups = p.kblocks / p.pairs;
-    k0 = (int)((long long)groups * sp / p.splits) * p.pairs;
-    k1 = (int)((long long)groups * (sp + 1) / p.splits) * p.pairs;
+  auto k_range = [&](int sp, int& k0, int& k1) {  // all parts of a tile
+    const int groups = p.kblocks / p.planes;
+    k0 = (int)((long long)groups * sp / p.splits) * p.planes;
+    k1 = (int)((long long)groups * (sp + 1) / p.splits) * p.planes;
   };
 
   if (threadIdx.x == 0) {
@@ -266,26 +284,25 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
         unit_at(p, u, pt, qt, sp);
         k_range(sp, k0, k1);
         const int prow = pt * 128 * CG + (int)rank * 128, qrow = qt * BN + (int)rank * (BN / CG);
-        int r0 = k0 / p.pairs * kBox, j = 0;
+        int r0 = k0 / p.planes * kBox, j = 0;  // j counts the parts from the smallest
         for (int kb = k0; kb < k1; ++kb) {
           if (!ptx::mbar_wait(&empty[s], ph ^ 1, abort_flag)) { ok = false; break; }
           uint8_t* st = smem + s * kStage;
-          // parts of the pair (0 h, 1 m, 2 l), a digit per j: mm, hl, lh, hm, mh, hh
-          const int pa = p.pairs == 1 ? 0 : (0x010201 >> (4 * j)) & 3, pb = p.pairs == 1 ? 0 : (0x001021 >> (4 * j)) & 3;
+          const int part = p.planes - 1 - j;
           if (rank == 0) ptx::mbar_expect_tx(&full[s], CG * kStage);
           if (p.a_along_r) {
-            ptx::tma_load_3d<CG>(st, &tm_a, &full[s], r0, prow, pa);
+            ptx::tma_load_3d<CG>(st, &tm_a, &full[s], r0, prow, part);
           } else {
-            ptx::tma_load_3d<CG>(st, &tm_a, &full[s], prow, r0, pa);
-            ptx::tma_load_3d<CG>(st + 8192, &tm_a, &full[s], prow + 64, r0, pa);
+            ptx::tma_load_3d<CG>(st, &tm_a, &full[s], prow, r0, part);
+            ptx::tma_load_3d<CG>(st + 8192, &tm_a, &full[s], prow + 64, r0, part);
           }
           if (p.b_along_r) {
-            ptx::tma_load_3d<CG>(st + kA, &tm_b, &full[s], r0, qrow, pb);
+            ptx::tma_load_3d<CG>(st + kA, &tm_b, &full[s], r0, qrow, part);
           } else {
 #pragma unroll
-            for (int i = 0; i < BN / CG / 64; ++i) ptx::tma_load_3d<CG>(st + kA + i * 8192, &tm_b, &full[s], qrow + 64 * i, r0, pb);
+            for (int i = 0; i < BN / CG / 64; ++i) ptx::tma_load_3d<CG>(st + kA + i * 8192, &tm_b, &full[s], qrow + 64 * i, r0, part);
           }
-          if (++j == p.pairs) {
+          if (++j == p.planes) {
             j = 0;
             r0 += kBox;
           }
@@ -318,17 +335,45 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
           ptx::tc_fence_after();
           const uint32_t d = tmem + acc * BN;
           uint32_t add = 0;
-          for (; kb < end; ++kb) {
-            if (!ptx::mbar_wait(&full[s], ph, abort_flag)) { ok = false; break; }
-            ptx::tc_fence_after();
-            const uint32_t a16 = ptx::smem_u32(smem + s * kStage) >> 4, b16 = a16 + (kA >> 4);
+          auto products = [&](uint32_t a16, uint32_t b16) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
               ptx::mma_f16_cg<CG>(d, hi_a | (uint64_t)(a16 + k * ka), hi_b | (uint64_t)(b16 + k * kbs), idesc, add);
               add = 1;
             }
-            ptx::mma_commit_cg<CG>(&empty[s]);
-            if (++s == kStages) { s = 0; ph ^= 1; }
+          };
+          if (kSegments && p.planes == 3) {  // parts l, m, h in three stages, each given back after its last use, in the order they are filled again
+            for (; ok && kb < end; kb += 3) {
+              uint32_t st[3], at[3];
+#pragma unroll
+              for (int i = 0; i < 3; ++i) {
+                st[i] = s;
+                at[i] = ptx::smem_u32(smem + s * kStage) >> 4;
+                ok = ok && ptx::mbar_wait(&full[s], ph, abort_flag);
+                if (++s == kStages) { s = 0; ph ^= 1; }
+              }
+              if (!ok) break;
+              ptx::tc_fence_after();
+              constexpr uint32_t kB16 = kA >> 4;
+              products(at[0], at[2] + kB16);  // l h
+              products(at[2], at[0] + kB16);  // h l
+              ptx::mma_commit_cg<CG>(&empty[st[0]]);
+              products(at[1], at[1] + kB16);  // m m
+              products(at[2], at[1] + kB16);  // h m
+              products(at[1], at[2] + kB16);  // m h
+              ptx::mma_commit_cg<CG>(&empty[st[1]]);
+              products(at[2], at[2] + kB16);  // h h
+              ptx::mma_commit_cg<CG>(&empty[st[2]]);
+            }
+          } else {
+            for (; kb < end; ++kb) {
+              if (!ptx::mbar_wait(&full[s], ph, abort_flag)) { ok = false; break; }
+              ptx::tc_fence_after();
+              const uint32_t a16 = ptx::smem_u32(smem + s * kStage) >> 4;
+              products(a16, a16 + (kA >> 4));
+              ptx::mma_commit_cg<CG>(&empty[s]);
+              if (++s == kStages) { s = 0; ph ^= 1; }
+            }
           }
           if (ok) ptx::mma_commit_cg<CG>(&tfull[acc]);
           if (++acc == 2) { acc = 0; aph ^= 1; }
@@ -340,7 +385,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
     constexpr int CH = 128 / sizeof(T), kChunks = BN / 2 / CH;
     const int w = warp - 2, half = w >> 2, lg = warp & 3;
     WayOut<T> out;
-    out.stage_p = staging + w * 8192;
+    out.stage_p = staging + w * kTiles<T> * 4096;
     out.stage = ptx::smem_u32(out.stage_p);
     out.rbar = rbars + 2 * w;
     out.rphase = 0;
@@ -354,7 +399,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
       k_range(sp, k0, k1);
       const int row0 = pt * 128 * CG + (int)rank * 128 + lg * 32, col0 = qt * BN + half * (BN / 2);
       const uint32_t taddr = tmem + ((uint32_t)(lg * 32) << 16) + half * (BN / 2);
-      out.fetch(p, &tm_r, out.turn & 1, row0, col0);
+      out.fetch(p, &tm_r, out.turn & (kTiles<T> - 1), row0, col0);
       if constexpr (kSegments) {
         float sum[BN / 2];
 #pragma unroll
@@ -433,12 +478,12 @@ int launch(const GemmProblem& g, const Epilogue& e, float* part, int splits) {
   GemmParams p{};
   p.P = g.P;
   p.Q = g.Q;
-  p.pairs = g.planes == 3 ? 6 : 1;
-  p.kblocks = (g.R + kBox - 1) / kBox * p.pairs;
+  p.planes = g.planes;
+  p.kblocks = (g.R + kBox - 1) / kBox * p.planes;
   p.tiles_p = (g.P + 128 * CG - 1) / (128 * CG);
   p.tiles_q = (g.Q + BN - 1) / BN;
   p.splits = splits;
-  p.seg = p.pairs == 6 ? 6 : 4;
+  p.seg = p.planes == 3 ? 3 : 8;  // 24 products of 16, or 32: errors of 1.5e-7 and 3e-7 (the running sum loses about 2^-25 of itself at each)
   p.a_along_r = g.A.along_r;
   p.b_along_r = g.B.along_r;
   p.e = e;
@@ -469,13 +514,13 @@ int launch(const GemmProblem& g, const Epilogue& e, float* part, int splits) {
   if (dev < 0 || dev >= 64) return NF_EUNSUPPORTED;
   auto k = gemm_tc_kernel<CG, BN, T>;
   if (!ready[dev]) {
-    NF_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmem<CG, BN>));
+    NF_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmem<CG, BN, T>));
     ready[dev] = true;
   }
   const long units = (long)p.tiles_p * p.tiles_q * splits;
   const int most = nf_tc_sm_count() / CG;
   const unsigned grid = (unsigned)((units < most ? units : most) * CG);
-  nf_launch_cluster(k, grid, kGemmThreads, kGemmSmem<CG, BN>, CG, ta, tb, tc, tr, tp, p);
+  nf_launch_cluster(k, grid, kGemmThreads, kGemmSmem<CG, BN, T>, CG, ta, tb, tc, tr, tp, p);
   NF_LAUNCHED();
   return NF_OK;
 }
@@ -487,10 +532,9 @@ bool large_tiles(int P, int Q) { return (long)((P + 255) / 256) * ((Q + 255) / 2
 int nf_gemm_splits(int P, int Q, int R, int planes) {
   if (large_tiles(P, Q)) return 1;
   const long tiles = (long)((P + 127) / 128) * ((Q + 127) / 128);
-  long s = 148 / tiles, most = ((long)R + 255) / 256;
+  long s = 148 / tiles, most = (long)R * (planes == 3 ? 6 : 1) / 1024;  // 16 steps of 64 at least: joining costs a launch and the partial sums' traffic
   if (s > most) s = most;
   if (s > 64) s = 64;
-  (void)planes;
   return s < 1 ? 1 : (int)s;
 }
 

@@ -24,28 +24,37 @@ __device__ __forceinline__ void finish(const Epilogue& e, size_t at, int q, floa
   stf(reinterpret_cast<T*>(e.out), at, nf_act_value<T>(v, e.act));
 }
 
-// 64 x 64 results per block, 4 x 4 per thread, 16 steps of r at a time; sa_p, sa_r: element strides of A.  gridDim.z > 1: each z sums a
+// fp32 on the CUDA cores, for products too small for the tensor cores: 64 x 64 results per block, 4 x 4 per thread, 16 steps of r at a time; sa_p, sa_r: element strides of A.  gridDim.z > 1: each z sums a
 // range of r into part[z][P][Q].
-template <typename T>
-__global__ void __launch_bounds__(256) gemm_simple_kernel(const T* __restrict__ A, size_t sa_p, size_t sa_r, const T* __restrict__ B, size_t sb_q,
+__global__ void __launch_bounds__(256) gemm_simple_kernel(const float* __restrict__ A, size_t sa_p, size_t sa_r, const float* __restrict__ B, size_t sb_q,
                                                           size_t sb_r, int P, int Q, int R, float* part, const Epilogue e) {
   nf_pdl_begin();
   __shared__ float As[16][68], Bs[16][68];
   const int p0 = blockIdx.x * 64, q0 = blockIdx.y * 64;
   const int r_lo = (int)((long long)R * blockIdx.z / gridDim.z), r_hi = (int)((long long)R * (blockIdx.z + 1) / gridDim.z);
   const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-  float acc[4][4] = {};
-  for (int r0 = r_lo; r0 < r_hi; r0 += 16) {
+  float acc[4][4] = {}, na[4], nb[4];  // the next step's operands are on their way while this one's are multiplied
+  auto fetch = [&](int r0) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int l = threadIdx.x + 256 * i;
       // neighbouring threads along whichever direction is contiguous
       const int pa = sa_r == 1 ? l / 16 : l % 64, ra = sa_r == 1 ? l % 16 : l / 64;
-      As[ra][pa] = p0 + pa < P && r0 + ra < r_hi ? ldf(A, (size_t)(p0 + pa) * sa_p + (size_t)(r0 + ra) * sa_r) : 0.f;
+      na[i] = p0 + pa < P && r0 + ra < r_hi ? A[(size_t)(p0 + pa) * sa_p + (size_t)(r0 + ra) * sa_r] : 0.f;
       const int qb = sb_r == 1 ? l / 16 : l % 64, rb = sb_r == 1 ? l % 16 : l / 64;
-      Bs[rb][qb] = q0 + qb < Q && r0 + rb < r_hi ? ldf(B, (size_t)(q0 + qb) * sb_q + (size_t)(r0 + rb) * sb_r) : 0.f;
+      nb[i] = q0 + qb < Q && r0 + rb < r_hi ? B[(size_t)(q0 + qb) * sb_q + (size_t)(r0 + rb) * sb_r] : 0.f;
+    }
+  };
+  fetch(r_lo);
+  for (int r0 = r_lo; r0 < r_hi; r0 += 16) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int l = threadIdx.x + 256 * i;
+      As[sa_r == 1 ? l % 16 : l / 64][sa_r == 1 ? l / 16 : l % 64] = na[i];
+      Bs[sb_r == 1 ? l % 16 : l / 64][sb_r == 1 ? l / 16 : l % 64] = nb[i];
     }
     __syncthreads();
+    if (r0 + 16 < r_hi) fetch(r0 + 16);
 #pragma unroll
     for (int k = 0; k < 16; ++k) {
       float a[4], b[4];
@@ -70,7 +79,7 @@ __global__ void __launch_bounds__(256) gemm_simple_kernel(const T* __restrict__ 
       if (gridDim.z > 1)
         part[(size_t)blockIdx.z * P * Q + at] = acc[i][j];
       else
-        finish<T>(e, at, q, acc[i][j]);
+        finish<float>(e, at, q, acc[i][j]);
     }
 }
 
@@ -84,22 +93,113 @@ __global__ void __launch_bounds__(256) gemm_join_kernel(const float* __restrict_
   finish<T>(e, i, (int)(i % Q), (float)s);
 }
 
-// part[block][n]: sums of g over a range of rows
+// A few rows of x (MR at most) through weights contiguous along r: the weights are all the traffic.  A block of 128 threads takes kThinRows
+// weight rows; its threads share a row in 16-byte pieces, so that a block has 128 * kThinRows * 16 bytes on their way at a time, and each
+// piece of x serves kThinRows rows of weights.  Pairs of neighbouring products are added in one packed multiply-add; threads' sums meet by shuffles
+// and shared memory.
+constexpr int kThinRows = 4;
+// Up to four rows of bf16, eight of fp32: beyond, the tensor cores take the product sooner (8 x 8192 x 4096 bf16 38 us here, 18 there)
+template <typename T> constexpr int kThinMost = sizeof(T) == 4 ? 8 : 4;
+
+template <typename T, int MR>
+__global__ void __launch_bounds__(128) thin_kernel(const T* __restrict__ x, const T* __restrict__ w, int M, int N, int K, const Epilogue e) {
+  nf_pdl_begin();
+  constexpr int V = 16 / sizeof(T), NP = V / 2;
+  __shared__ float sm[4][kThinRows * MR];
+  const int n0 = blockIdx.x * kThinRows;
+  f32x2 acc[kThinRows][MR];
+#pragma unroll
+  for (int j = 0; j < kThinRows; ++j)
+#pragma unroll
+    for (int m = 0; m < MR; ++m) acc[j][m] = 0;
+  auto pairs = [](const T* at, f32x2 (&v)[NP], bool stream) {
+    if constexpr (sizeof(T) == 2) {
+      const uint4 u = stream ? __ldcs(reinterpret_cast<const uint4*>(at)) : __ldg(reinterpret_cast<const uint4*>(at));
+      const uint32_t q[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = nf_pack2(__uint_as_float(q[i] << 16), __uint_as_float(q[i] & 0xffff0000u));
+    } else {
+      const float4 u = stream ? __ldcs(reinterpret_cast<const float4*>(at)) : __ldg(reinterpret_cast<const float4*>(at));
+      v[0] = nf_pack2(u.x, u.y);
+      v[1] = nf_pack2(u.z, u.w);
+    }
+  };
+#pragma unroll 2
+  for (int k = threadIdx.x * V; k < K; k += 128 * V) {
+    f32x2 b[kThinRows][NP];
+#pragma unroll
+    for (int j = 0; j < kThinRows; ++j) pairs(w + (size_t)min(n0 + j, N - 1) * K + k, b[j], true);  // rows beyond N: the last one again, not stored
+#pragma unroll
+    for (int m = 0; m < MR; ++m) {
+      f32x2 a[NP];
+      pairs(x + (size_t)min(m, M - 1) * K + k, a, false);
+#pragma unroll
+      for (int j = 0; j < kThinRows; ++j)
+#pragma unroll
+        for (int i = 0; i < NP; ++i) acc[j][m] = nf_fma2(a[i], b[j][i], acc[j][m]);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < kThinRows; ++j)
+#pragma unroll
+    for (int m = 0; m < MR; ++m) {
+      float lo, hi;
+      nf_unpack2(acc[j][m], lo, hi);
+      float v = lo + hi;
+#pragma unroll
+      for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+      if (threadIdx.x % 32 == 0) sm[threadIdx.x / 32][m * kThinRows + j] = v;
+    }
+  __syncthreads();
+  if (threadIdx.x < kThinRows * MR) {
+    const int m = threadIdx.x / kThinRows, n = n0 + threadIdx.x % kThinRows;
+    if (m < M && n < N) finish<T>(e, (size_t)m * N + n, n, (sm[0][threadIdx.x] + sm[1][threadIdx.x]) + (sm[2][threadIdx.x] + sm[3][threadIdx.x]));
+  }
+}
+
 template <typename T>
+int thin_product(const T* x, const T* w, int M, int N, int K, const Epilogue& e) {
+  auto k = M == 1 ? thin_kernel<T, 1> : M == 2 ? thin_kernel<T, 2> : M <= 4 ? thin_kernel<T, 4> : thin_kernel<T, kThinMost<T>>;
+  nf_launch(k, (unsigned)((N + kThinRows - 1) / kThinRows), 128, 0, x, w, M, N, K, e);
+  NF_LAUNCHED();
+  return NF_OK;
+}
+
+// part[block][n]: sums of g over a range of rows.  V columns per thread (16 bytes of a row where rows are made of such pieces), 32 threads along a
+// row, eight rows at a time.
+template <typename T, int V>
 __global__ void __launch_bounds__(256) column_sums_kernel(const T* __restrict__ g, int M, int N, float* __restrict__ part) {
   nf_pdl_begin();
-  __shared__ float sm[8][32];
-  const int tx = threadIdx.x % 32, ty = threadIdx.x / 32, n = blockIdx.y * 32 + tx;
+  __shared__ float sm[8][32 * V + 1];
+  const int tx = threadIdx.x % 32, ty = threadIdx.x / 32, n = (blockIdx.y * 32 + tx) * V;
   const int m0 = (int)((long long)M * blockIdx.x / gridDim.x), m1 = (int)((long long)M * (blockIdx.x + 1) / gridDim.x);
-  float s = 0;
-  if (n < N)
-    for (int m = m0 + ty; m < m1; m += 8) s += ldf(g, (size_t)m * N + n);
-  sm[ty][tx] = s;
-  __syncthreads();
-  if (ty == 0 && n < N) {
+  float s[V];
 #pragma unroll
-    for (int k = 1; k < 8; ++k) s += sm[k][tx];
-    part[(size_t)blockIdx.x * N + n] = s;
+  for (int e = 0; e < V; ++e) s[e] = 0.f;
+  if (n < N) {
+#pragma unroll 4
+    for (int m = m0 + ty; m < m1; m += 8) {
+      const T* at = g + (size_t)m * N + n;
+      if constexpr (V == 8) {
+        float v[8];
+        ld8(at, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] += v[e];
+      } else {
+        s[0] += ldf(at, 0);
+      }
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < V; ++e) sm[ty][tx * V + e] = s[e];
+  __syncthreads();
+  for (int i = threadIdx.x; i < 32 * V; i += 256) {
+    const int c = blockIdx.y * 32 * V + i;
+    if (c >= N) break;
+    float v = sm[0][i];
+#pragma unroll
+    for (int k = 1; k < 8; ++k) v += sm[k][i];
+    part[(size_t)blockIdx.x * N + c] = v;
   }
 }
 
@@ -162,10 +262,9 @@ struct Product {
   int b_len() const { return b_along_r ? R : Q; }
 };
 
-bool on_tensor_cores(int dtype, const Product& d) {
-  const double work = (double)d.P * d.Q * d.R;
-  return work >= (dtype == NF_BF16 ? 2097152.0 : 134217728.0);
-}
+// bf16: always (a 128 x 64 x 10 product took 6 us there and 10 us on the CUDA cores).  fp32: from 2^26 multiply-adds on, where what
+// cutting the operands into parts costs is earned back (256 x 256 x 256 16 us there, 9 us here; 512 x 512 x 512 17 us and 24 us).
+bool on_tensor_cores(int dtype, const Product& d) { return dtype == NF_BF16 || (double)d.P * d.Q * d.R >= 67108864.0; }
 bool needs_copy(int dtype, int len) { return dtype == NF_F32 || len % 8; }
 size_t copy_bytes(int dtype, int rows, int len) {
   return needs_copy(dtype, len) ? nf_align_up((size_t)rows * pad8(len) * 2 * (dtype == NF_F32 ? 3 : 1), 256) : 0;
@@ -174,7 +273,7 @@ size_t copy_bytes(int dtype, int rows, int len) {
 int simple_splits(int P, int Q, int R) {
   const long tiles = (long)((P + 63) / 64) * ((Q + 63) / 64);
   long s = 296 / tiles;
-  if (s > R / 256) s = R / 256;
+  if (s > R / 64) s = R / 64;  // four steps of 16 at least
   return s < 1 ? 1 : (int)s;
 }
 
@@ -194,14 +293,13 @@ int join(const float* part, int splits, int P, int Q, const Epilogue& e) {
   return NF_OK;
 }
 
-template <typename T>
-int simple_product(const Product& d, const void* A, const void* B, float* part, const Epilogue& e) {
+int simple_product(const Product& d, const float* A, const float* B, float* part, const Epilogue& e) {
   const int splits = simple_splits(d.P, d.Q, d.R);
   const size_t la = d.a_len(), lb = d.b_len();
-  nf_launch(gemm_simple_kernel<T>, dim3((d.P + 63) / 64, (d.Q + 63) / 64, splits), 256, 0, (const T*)A, d.a_along_r ? la : 1, d.a_along_r ? 1 : la,
-            (const T*)B, d.b_along_r ? lb : 1, d.b_along_r ? 1 : lb, d.P, d.Q, d.R, part, e);
+  nf_launch(gemm_simple_kernel, dim3((d.P + 63) / 64, (d.Q + 63) / 64, splits), 256, 0, A, d.a_along_r ? la : 1, d.a_along_r ? 1 : la,
+            B, d.b_along_r ? lb : 1, d.b_along_r ? 1 : lb, d.P, d.Q, d.R, part, e);
   NF_LAUNCHED();
-  return splits > 1 ? join<T>(part, splits, d.P, d.Q, e) : NF_OK;
+  return splits > 1 ? join<float>(part, splits, d.P, d.Q, e) : NF_OK;
 }
 
 template <typename T>
@@ -223,7 +321,11 @@ template <typename T>
 int product(const Product& d, const void* A, const void* B, void* scratch, const Epilogue& e) {
   const int dtype = sizeof(T) == 4 ? NF_F32 : NF_BF16;
   if ((d.Q + 63) / 64 > 65535) return NF_EUNSUPPORTED;
-  if (!on_tensor_cores(dtype, d)) return simple_product<T>(d, A, B, (float*)scratch, e);
+  if (d.P <= kThinMost<T> && d.a_along_r && d.b_along_r && d.R % (16 / (int)sizeof(T)) == 0)
+    return thin_product<T>((const T*)A, (const T*)B, d.P, d.Q, d.R, e);
+  if constexpr (sizeof(T) == 4) {
+    if (!on_tensor_cores(dtype, d)) return simple_product(d, (const float*)A, (const float*)B, (float*)scratch, e);
+  }
   char* s = (char*)scratch;
   GemmProblem g{};
   g.P = d.P; g.Q = d.Q; g.R = d.R;
@@ -236,7 +338,11 @@ int product(const Product& d, const void* A, const void* B, void* scratch, const
   return rc == NF_OK && splits > 1 ? join<T>((const float*)s, splits, d.P, d.Q, e) : rc;
 }
 
-int sum_blocks(int M) { return M < 148 * 8 ? (M + 7) / 8 : 148; }
+// Ranges of rows for the column sums: four blocks per SM, at least 32 rows each
+int sum_blocks(int M, int N) {
+  const int V = N % 8 == 0 ? 8 : 1, cols = (N + 32 * V - 1) / (32 * V), want = (592 + cols - 1) / cols, most = (M + 31) / 32;
+  return M <= 512 ? 1 : want < most ? want : most;  // few rows: one range, whose sums are the result
+}
 
 bool sizes_ok(int dtype, int M, int K, int N) { return (dtype == NF_F32 || dtype == NF_BF16) && M >= 1 && K >= 1 && N >= 1; }
 
@@ -253,7 +359,7 @@ extern "C" size_t nf_linear_scratch_bytes(int dtype, int M, int K, int N) {
     const size_t n = product_bytes(dtype, d);
     if (n > b) b = n;
   }
-  return b + (size_t)sum_blocks(M) * N * 4 + 256;
+  return b + (size_t)sum_blocks(M, N) * N * 4 + 256;
 }
 
 extern "C" int nf_linear_forward(int dtype, const void* x, const void* w, const float* bias, const void* residual, int M, int K, int N, int act,
@@ -295,14 +401,18 @@ extern "C" int nf_linear_wgrad(int dtype, const void* x, const void* g, int M, i
   const Product d = wgrad_of(M, K, N);
   const int rc = dtype == NF_F32 ? product<float>(d, g, x, scratch, e) : product<bf16>(d, g, x, scratch, e);
   if (rc != NF_OK || !db) return rc;
-  float* part = (float*)scratch;  // the product's partial sums have been read by now
-  const dim3 grid(sum_blocks(M), (N + 31) / 32);
-  if (dtype == NF_F32)
-    nf_launch(column_sums_kernel<float>, grid, 256, 0, (const float*)g, M, N, part);
-  else
-    nf_launch(column_sums_kernel<bf16>, grid, 256, 0, (const bf16*)g, M, N, part);
+  const int blocks = sum_blocks(M, N);
+  float* part = blocks > 1 ? (float*)scratch : db;  // the product's partial sums have been read by now
+  if ((N + 31) / 32 > 65535) return NF_EUNSUPPORTED;
+  if (dtype == NF_F32) {
+    if (N % 8 == 0) nf_launch(column_sums_kernel<float, 8>, dim3(blocks, (N + 255) / 256), 256, 0, (const float*)g, M, N, part);
+    else nf_launch(column_sums_kernel<float, 1>, dim3(blocks, (N + 31) / 32), 256, 0, (const float*)g, M, N, part);
+  } else {
+    if (N % 8 == 0) nf_launch(column_sums_kernel<bf16, 8>, dim3(blocks, (N + 255) / 256), 256, 0, (const bf16*)g, M, N, part);
+    else nf_launch(column_sums_kernel<bf16, 1>, dim3(blocks, (N + 31) / 32), 256, 0, (const bf16*)g, M, N, part);
+  }
   NF_LAUNCHED();
-  return nf_k_sum_parts(part, sum_blocks(M), N, db, true);
+  return blocks > 1 ? nf_k_sum_parts(part, blocks, N, db, true) : NF_OK;
 }
 
 extern "C" int nf_act_backward(int dtype, int act, const void* saved, const void* dy, long long n, void* g) {
