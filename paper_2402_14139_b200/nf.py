@@ -561,23 +561,36 @@ def nf_conv3x3_wgrad_static(dtype, x, g, stride, dw):
            "nf_conv3x3_wgrad_static")
 
 
-def _storage(dtype):
-    import torch
-    if dtype not in (NF_F32, NF_BF16):
+_TYPES = {}      # nf_dtype -> torch dtype, and the other types the calls below check; filled on first use: importing this module imports no torch
+
+
+def _call(dtype, *sizes):
+    """For a call on tensors of this nf_dtype: (torch dtype, torch.float32, current device).  Refuses sizes that a C int does not hold."""
+    if not _TYPES:
+        import torch
+        _TYPES.update({NF_F32: torch.float32, NF_BF16: torch.bfloat16, "i32": torch.int32, "i64": torch.int64, "u8": torch.uint8,
+                       "device": torch.cuda.current_device if torch.cuda.is_available() else lambda: -2})
+    if dtype != NF_F32 and dtype != NF_BF16:
         raise NfError(f"dtype: NF_F32 or NF_BF16, not {dtype!r}")
-    return torch.float32 if dtype == NF_F32 else torch.bfloat16
+    for v in sizes:
+        if v > 0x7fffffff:
+            raise NfError(f"size {v}: beyond 2^31 - 1")
+    return _TYPES[dtype], _TYPES[NF_F32], _TYPES["device"]()
 
 
-def _tensor(what, t, dtype, shape, host_ok=False):
-    """Address of a dense tensor of this type and shape on the current device (host_ok: or in pinned host memory)."""
-    import torch
+def _tensor(what, t, dtype, shape, dev, host_ok=False):
+    """Address of a dense tensor of this type and shape on device `dev`, the current one (host_ok: or in pinned host memory)."""
+    if t.dtype is dtype and t.shape == shape and t.is_contiguous() and (t.get_device() == dev or (host_ok and t.is_pinned())):
+        return t.data_ptr()
     if t.dtype is not dtype or t.shape != shape:
         raise NfError(f"{what}: want {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
     if not t.is_contiguous():
         raise NfError(f"{what}: not dense")
-    if not (t.is_cuda and t.get_device() == torch.cuda.current_device()) and not (host_ok and t.is_pinned()):
-        raise NfError(f"{what}: not on the current CUDA device")
-    return t.data_ptr()
+    raise NfError(f"{what}: not on the current CUDA device")
+
+
+def _maybe(what, t, dtype, shape, dev):
+    return None if t is None else _tensor(what, t, dtype, shape, dev)
 
 
 def _choice(what, table, key):
@@ -586,25 +599,33 @@ def _choice(what, table, key):
     return table[key]
 
 
-def _param(what, t, shape):
-    import torch
-    return _tensor(what, t, torch.float32, shape)
+def _scratch(t, dev):
+    return _tensor("scratch", t, _TYPES["u8"], t.shape, dev), t.numel()
 
 
-def _scratch(what, t):
-    import torch
-    return _tensor(what, t, torch.uint8, t.shape), t.numel()
+def _matrix(what, t):
+    if t.dim() != 2:
+        raise NfError(f"{what}: want two dimensions, got {tuple(t.shape)}")
+    return t.shape
+
+
+def _images(x):
+    """(N, P, C) of [N, ..., C]: every dimension between is pixels."""
+    if x.dim() < 2:
+        raise NfError(f"x: want [N, ..., C], got {tuple(x.shape)}")
+    N, C_ = x.shape[0], x.shape[-1]
+    return N, x.numel() // (N * C_ or 1), C_
 
 
 def nf_group_norm_forward(dtype, x, gamma, beta, groups, eps, act, y, mean, rstd):
     """y = act(group_norm(x)): x, y [N, ..., C] of dtype (all dimensions between are pixels), gamma, beta float32 [C], act a key of
     ACTS; mean, rstd float32 [N, groups] are written for the backward pass."""
-    td = _storage(dtype)
-    N, C_ = x.shape[0], x.shape[-1]
-    P = x.numel() // max(1, N * C_)
-    _check(lib().nf_group_norm_forward(dtype, _tensor("x", x, td, x.shape), _param("gamma", gamma, (C_,)), _param("beta", beta, (C_,)), N, P, C_,
-                                       int(groups), float(eps), _choice("act", ACTS, act), _tensor("y", y, td, x.shape),
-                                       _param("mean", mean, (N, groups)), _param("rstd", rstd, (N, groups))), "nf_group_norm_forward")
+    N, P, C_ = _images(x)
+    td, f32, dev = _call(dtype, N, P, C_)
+    _check(lib().nf_group_norm_forward(dtype, _tensor("x", x, td, x.shape, dev), _tensor("gamma", gamma, f32, (C_,), dev),
+                                       _tensor("beta", beta, f32, (C_,), dev), N, P, C_, groups, eps, _choice("act", ACTS, act),
+                                       _tensor("y", y, td, x.shape, dev), _tensor("mean", mean, f32, (N, groups), dev),
+                                       _tensor("rstd", rstd, f32, (N, groups), dev)), "nf_group_norm_forward")
 
 
 def nf_group_norm_scratch_bytes(dtype, N, P, C_, groups) -> int:
@@ -614,13 +635,14 @@ def nf_group_norm_scratch_bytes(dtype, N, P, C_, groups) -> int:
 def nf_group_norm_backward(dtype, x, dy, gamma, beta, mean, rstd, act, scratch, dx, dgamma, dbeta):
     """dx, dgamma, dbeta from x, dy and what the forward pass left in mean and rstd [N, groups]; scratch: uint8 tensor of at least
     nf_group_norm_scratch_bytes(dtype, N, P, C, groups)."""
-    td = _storage(dtype)
-    N, C_ = x.shape[0], x.shape[-1]
-    P, groups = x.numel() // max(1, N * C_), mean.shape[-1]
-    _check(lib().nf_group_norm_backward(dtype, _tensor("x", x, td, x.shape), _tensor("dy", dy, td, x.shape), _param("gamma", gamma, (C_,)),
-                                        _param("beta", beta, (C_,)), _param("mean", mean, (N, groups)), _param("rstd", rstd, (N, groups)), N, P, C_,
-                                        groups, _choice("act", ACTS, act), *_scratch("scratch", scratch), _tensor("dx", dx, td, x.shape),
-                                        _param("dgamma", dgamma, (C_,)), _param("dbeta", dbeta, (C_,))), "nf_group_norm_backward")
+    N, P, C_ = _images(x)
+    td, f32, dev = _call(dtype, N, P, C_)
+    groups, c = _matrix("mean", mean)[1], (C_,)
+    _check(lib().nf_group_norm_backward(dtype, _tensor("x", x, td, x.shape, dev), _tensor("dy", dy, td, x.shape, dev),
+                                        _tensor("gamma", gamma, f32, c, dev), _tensor("beta", beta, f32, c, dev),
+                                        _tensor("mean", mean, f32, (N, groups), dev), _tensor("rstd", rstd, f32, (N, groups), dev), N, P, C_, groups,
+                                        _choice("act", ACTS, act), *_scratch(scratch, dev), _tensor("dx", dx, td, x.shape, dev),
+                                        _tensor("dgamma", dgamma, f32, c, dev), _tensor("dbeta", dbeta, f32, c, dev)), "nf_group_norm_backward")
 
 
 def nf_linear_scratch_bytes(dtype, M, K, N) -> int:
@@ -631,72 +653,69 @@ def nf_linear_forward(dtype, x, w, bias, residual, act, scratch, pre, y):
     """y = act(x w^T + bias + residual): x [M, K], w [N, K], residual, pre, y [M, N] of dtype, bias float32 [N]; bias, residual and pre
     (the value before the activation, for the backward pass of SiLU and GELU) may be None; scratch: uint8 tensor of at least
     nf_linear_scratch_bytes(dtype, M, K, N)."""
-    td = _storage(dtype)
-    (M, K), N = x.shape, w.shape[0]
-    _check(lib().nf_linear_forward(dtype, _tensor("x", x, td, (M, K)), _tensor("w", w, td, (N, K)),
-                                   None if bias is None else _param("bias", bias, (N,)),
-                                   None if residual is None else _tensor("residual", residual, td, (M, N)), M, K, N, _choice("act", ACTS, act),
-                                   *_scratch("scratch", scratch), None if pre is None else _tensor("pre", pre, td, (M, N)),
-                                   _tensor("y", y, td, (M, N))), "nf_linear_forward")
+    (M, K), N = _matrix("x", x), _matrix("w", w)[0]
+    td, f32, dev = _call(dtype, M, K, N)
+    out = (M, N)
+    _check(lib().nf_linear_forward(dtype, _tensor("x", x, td, (M, K), dev), _tensor("w", w, td, (N, K), dev), _maybe("bias", bias, f32, (N,), dev),
+                                   _maybe("residual", residual, td, out, dev), M, K, N, _choice("act", ACTS, act), *_scratch(scratch, dev),
+                                   _maybe("pre", pre, td, out, dev), _tensor("y", y, td, out, dev)), "nf_linear_forward")
 
 
 def nf_act_backward(dtype, act, saved, dy, g):
     """g = dy * act'(saved), elementwise; saved: the pre-activation, or for ReLU the output.  g may be dy or saved."""
-    td = _storage(dtype)
-    _check(lib().nf_act_backward(dtype, _choice("act", ACTS, act), _tensor("saved", saved, td, dy.shape), _tensor("dy", dy, td, dy.shape), dy.numel(),
-                                 _tensor("g", g, td, dy.shape)), "nf_act_backward")
+    td, _, dev = _call(dtype)
+    _check(lib().nf_act_backward(dtype, _choice("act", ACTS, act), _tensor("saved", saved, td, dy.shape, dev), _tensor("dy", dy, td, dy.shape, dev),
+                                 dy.numel(), _tensor("g", g, td, dy.shape, dev)), "nf_act_backward")
 
 
 def nf_linear_dgrad(dtype, g, w, scratch, dx):
-    """dx = g w: g [M, N], w [N, K], dx [M, K] of dtype."""
-    td = _storage(dtype)
-    M, (N, K) = g.shape[0], w.shape
-    _check(lib().nf_linear_dgrad(dtype, _tensor("g", g, td, (M, N)), _tensor("w", w, td, (N, K)), M, K, N, *_scratch("scratch", scratch),
-                                 _tensor("dx", dx, td, (M, K))), "nf_linear_dgrad")
+    """dx = g w: g [M, N], w [N, K], dx [M, K] of dtype; scratch as for nf_linear_forward."""
+    M, (N, K) = _matrix("g", g)[0], _matrix("w", w)
+    td, _, dev = _call(dtype, M, K, N)
+    _check(lib().nf_linear_dgrad(dtype, _tensor("g", g, td, (M, N), dev), _tensor("w", w, td, (N, K), dev), M, K, N, *_scratch(scratch, dev),
+                                 _tensor("dx", dx, td, (M, K), dev)), "nf_linear_dgrad")
 
 
 def nf_linear_wgrad(dtype, x, g, scratch, dw, db=None):
-    """dw = g^T x (float32 [N, K]) and, if db is given, the column sums of g (float32 [N]): x [M, K], g [M, N] of dtype."""
-    td = _storage(dtype)
-    (M, K), N = x.shape, g.shape[1]
-    _check(lib().nf_linear_wgrad(dtype, _tensor("x", x, td, (M, K)), _tensor("g", g, td, (M, N)), M, K, N, *_scratch("scratch", scratch),
-                                 _param("dw", dw, (N, K)), None if db is None else _param("db", db, (N,))), "nf_linear_wgrad")
+    """dw = g^T x (float32 [N, K]) and, if db is given, the column sums of g (float32 [N]): x [M, K], g [M, N] of dtype; scratch as for
+    nf_linear_forward."""
+    (M, K), N = _matrix("x", x), _matrix("g", g)[1]
+    td, f32, dev = _call(dtype, M, K, N)
+    _check(lib().nf_linear_wgrad(dtype, _tensor("x", x, td, (M, K), dev), _tensor("g", g, td, (M, N), dev), M, K, N, *_scratch(scratch, dev),
+                                 _tensor("dw", dw, f32, (N, K), dev), _maybe("db", db, f32, (N,), dev)), "nf_linear_wgrad")
 
 
 def nf_dropout(dtype, x, p, seed, offset, y, offset_dev=None):
     """y = x / (1 - p) where the generator keeps an element, else 0; the gradient is the same call on dy.  seed, offset: 64-bit integers;
     offset_dev: int64 tensor of one element on the device that is added to offset (advance it inside a recorded step).  y may be x."""
-    import torch
-    td = _storage(dtype)
-    m64 = (1 << 64) - 1
-    _check(lib().nf_dropout(dtype, _tensor("x", x, td, x.shape), x.numel(), float(p), int(seed) & m64, int(offset) & m64,
-                            None if offset_dev is None else _tensor("offset_dev", offset_dev, torch.int64, (1,)), _tensor("y", y, td, x.shape)),
-           "nf_dropout")
+    td, _, dev = _call(dtype)
+    _check(lib().nf_dropout(dtype, _tensor("x", x, td, x.shape, dev), x.numel(), p, seed & 0xffffffffffffffff, offset & 0xffffffffffffffff,
+                            _maybe("offset_dev", offset_dev, _TYPES["i64"], (1,), dev), _tensor("y", y, td, x.shape, dev)), "nf_dropout")
 
 
 def nf_cache_quantize(fmt, dtype, x, group, codes, scales):
     """Rows of x [rows, ...] of dtype into the 8-bit cache: codes uint8 of x's shape, scales float32 [rows, ceil(row elements / group)];
     fmt a key of CACHE_FORMATS, group 32, 64 or 128."""
-    import torch
     rows = x.shape[0]
-    E = x.numel() // max(1, rows)
-    _check(lib().nf_cache_quantize(_choice("format", CACHE_FORMATS, fmt), dtype, _tensor("x", x, _storage(dtype), x.shape), rows, E, int(group),
-                                   _tensor("codes", codes, torch.uint8, x.shape), _param("scales", scales, (rows, -(-E // int(group))))),
-           "nf_cache_quantize")
+    td, f32, dev = _call(dtype, rows)
+    E = x.numel() // (rows or 1)
+    _check(lib().nf_cache_quantize(_choice("format", CACHE_FORMATS, fmt), dtype, _tensor("x", x, td, x.shape, dev), rows, E, group,
+                                   _tensor("codes", codes, _TYPES["u8"], x.shape, dev),
+                                   _tensor("scales", scales, f32, (rows, -(-E // (group or 1))), dev)), "nf_cache_quantize")
 
 
 def nf_cache_gather_quantized(fmt, codes, scales, cache_labels, idx, group, dtype, out, out_labels):
     """out[i] = row idx[i] of the 8-bit cache, as dtype, and labels likewise (both label tensors or neither).  codes [rows, ...], scales and
     cache_labels may lie in pinned host memory; idx int32.  Indices outside the cache as in nf_cache_gather."""
-    import torch
     rows, count = codes.shape[0], idx.numel()
-    E = codes.numel() // max(1, rows)
+    td, f32, dev = _call(dtype, rows, count)
+    E, i32 = codes.numel() // (rows or 1), _TYPES["i32"]
     _check(lib().nf_cache_gather_quantized(
-        _choice("format", CACHE_FORMATS, fmt), _tensor("codes", codes, torch.uint8, codes.shape, True),
-        _tensor("scales", scales, torch.float32, (rows, -(-E // int(group))), True),
-        None if cache_labels is None else _tensor("cache_labels", cache_labels, torch.int32, (rows,), True), rows,
-        _tensor("idx", idx, torch.int32, (count,)), count, E, int(group), dtype, _tensor("out", out, _storage(dtype), (count,) + tuple(codes.shape[1:])),
-        None if out_labels is None else _tensor("out_labels", out_labels, torch.int32, (count,))), "nf_cache_gather_quantized")
+        _choice("format", CACHE_FORMATS, fmt), _tensor("codes", codes, _TYPES["u8"], codes.shape, dev, True),
+        _tensor("scales", scales, f32, (rows, -(-E // (group or 1))), dev, True),
+        None if cache_labels is None else _tensor("cache_labels", cache_labels, i32, (rows,), dev, True), rows, _tensor("idx", idx, i32, (count,), dev),
+        count, E, group, dtype, _tensor("out", out, td, (count,) + codes.shape[1:], dev), _maybe("out_labels", out_labels, i32, (count,), dev)),
+        "nf_cache_gather_quantized")
 
 
 def nf_selftest_bounded_wait(limit_ns: int, waited_ns_out):

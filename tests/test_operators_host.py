@@ -82,5 +82,11 @@ def test_binding_refuses_wrong_tensors(nf):
         nf.nf_dropout(7, x, 0.5, 1, 2, x)
     with pytest.raises(nf.NfError, match="act"):
         nf.nf_act_backward(nf.NF_F32, "tanh", x, x, x)
+    with pytest.raises(nf.NfError, match="two dimensions"):
+        nf.nf_linear_dgrad(nf.NF_F32, x, x[None], x, x)
+    with pytest.raises(nf.NfError, match="N, ..., C"):
+        nf.nf_group_norm_forward(nf.NF_F32, x[0], x[0], x[0], 1, 1e-5, "none", x[0], x[0], x[0])
+    with pytest.raises(nf.NfError, match="2\\^31"):
+        nf.nf_cache_quantize("int8", nf.NF_F32, torch.zeros(1).expand(1 << 31), 64, x, x)
     with pytest.raises(nf.NfError, match="format"):
         nf.nf_cache_quantize("int4", nf.NF_F32, x, 64, x, x)
