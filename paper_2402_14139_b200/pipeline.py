@@ -19,6 +19,10 @@ while batch k trains; the rows travel as raw bytes, so this tier is bit-identica
 block's parameters, momentum and running statistics leave the device as well (one .npz file per block, or host arrays):
 only the active block holds device memory, and load_block() brings a finished block back (for the selected exit model).
 
+With cache_format "int8" or "e4m3" the cache (tiers "hbm" and "host") holds 8-bit codes with one scale per `cache_group` elements
+(nf_cache_quantize as the cache fill produces a chunk, nf_cache_gather_quantized where a batch is assembled): half the memory and half the
+host-to-device traffic of bf16.  Rounding is the quantiser's, so results differ from the exact tiers by it.
+
 With a validation set, every trained layer is also evaluated as an exit point (nf_layer_predict on the
 validation activations that the earlier layers produced, nf_count_equal against the labels); the
 resulting (layer, accuracy, parameters) table goes through nf_select_exit.
@@ -124,6 +128,34 @@ def load_block(nf, wl, block_index, state):
     return layers, nf.Block(layers)
 
 
+class QuantizedCache:
+    """Activations of K samples as 8-bit codes [K, H, W, C] and scales [K, ceil(H W C / group)], on the device or in pinned host memory."""
+
+    def __init__(self, torch, fmt, group, shape, tdtype, device, host):
+        self.fmt, self.group, self.shape, self.tdtype, self.is_cuda = fmt, group, tuple(shape), tdtype, not host
+        n = -(-int(np.prod(shape[1:])) // group)
+        where = dict(pin_memory=True) if host else dict(device=device)
+        self.codes = torch.empty(self.shape, dtype=torch.uint8, **where)
+        self.scales = torch.empty((shape[0], n), dtype=torch.float32, **where)
+
+    def _dt(self, nf):
+        return nf.NF_F32 if self.tdtype.itemsize == 4 else nf.NF_BF16
+
+    def write(self, nf, start, x, stage):
+        """Rows start ... of the cache from the activations x on the device; stage: (codes, scales) buffers on the device where the
+        cache lies in host memory, else None."""
+        n = x.shape[0]
+        codes, scales = (self.codes[start:start + n], self.scales[start:start + n]) if stage is None else (stage[0][:n], stage[1][:n])
+        nf.nf_cache_quantize(self.fmt, self._dt(nf), x, self.group, codes, scales)
+        if stage is not None:
+            self.codes[start:start + n].copy_(codes, non_blocking=True)
+            self.scales[start:start + n].copy_(scales, non_blocking=True)
+
+    def read(self, nf, labels, idx, out, out_labels):
+        """out[i] = row idx[i], labels likewise (or both None)."""
+        nf.nf_cache_gather_quantized(self.fmt, self.codes, self.scales, labels, idx, self.group, self._dt(nf), out, out_labels)
+
+
 class _DiskBatches:
     """Batches drawn by index from a memory-mapped cache file: a reader thread copies the rows of the next batch into one
     of two pinned buffers (reads hit the page cache or the drive) while the current batch trains."""
@@ -168,16 +200,20 @@ def evaluate_exits(nf, torch, layers, N, val_cur, val_labels):
 
 
 def train_blockwise(nf, torch, wl, data, labels, epochs=1, lr=0.01, seed=1, log=None, val=None, cache="hbm", spill_dir=None,
-                    offload=None):
+                    offload=None, cache_format=None, cache_group=64):
     """data: device (or pinned host) tensor [K, H, W, C] of the first layer's dtype; labels: device int32 [K];
     cache: "hbm" keeps each block's output for all samples on the device, "host" in pinned host memory, "disk" in a
     memory-mapped file under spill_dir (bf16 workloads);
+    cache_format: None keeps the activations' type; "int8" or "e4m3" (not with "disk") stores 8-bit codes, one scale per cache_group elements, and
+    the cached output returned is a QuantizedCache;
     offload: None keeps nothing of a finished block but its cache; "host" stores its layers' state (Layer.export_state) in
     the block's record under "state"; a directory path writes block<i>.npz there and records the path;
     val: optional (device tensor [V, H, W, C], device int32 [V]) validation set.
     Returns (per-block records, the last block's cached output) and, with val, also the exit report
     dict(table=[(layer, accuracy, parameters)], selected=layer index)."""
     K = data.shape[0]
+    if cache_format is not None and cache == "disk":
+        raise ValueError('cache_format needs cache="hbm" or "host"')
     report = []
     cur = data
     labels_host = labels.cpu().numpy() if cache == "disk" else None
@@ -203,7 +239,10 @@ def train_blockwise(nf, torch, wl, data, labels, epochs=1, lr=0.01, seed=1, log=
             if k >= 2:
                 side.wait_event(free[k % 2])
             nf.nf_set_stream(side)
-            nf.nf_cache_gather(cur, labels, idx, bufs[k % 2][0], bufs[k % 2][1])
+            if isinstance(cur, QuantizedCache):
+                cur.read(nf, labels, idx, bufs[k % 2][0], bufs[k % 2][1])
+            else:
+                nf.nf_cache_gather(cur, labels, idx, bufs[k % 2][0], bufs[k % 2][1])
             ready[k % 2].record(side)
             nf.nf_set_stream(main)
             return idx        # kept alive by the caller until the gather has run
@@ -243,7 +282,7 @@ def train_blockwise(nf, torch, wl, data, labels, epochs=1, lr=0.01, seed=1, log=
             keep = keep[-3:]
         torch.cuda.synchronize()
         t_train = time.perf_counter() - t0
-        status = [L.status() for L in layers]
+        status = [L.status() for L in layers] + ([nf.nf_op_status()] if cache_format else [])
         if any(status):
             raise RuntimeError(f"block {bi}: device status {status}")
         # fill the cache: the block's output for every sample, in chunks of the block's batch size
@@ -256,13 +295,18 @@ def train_blockwise(nf, torch, wl, data, labels, epochs=1, lr=0.01, seed=1, log=
             out = np.lib.format.open_memmap(os.path.join(spill_dir, f"cache_block{bi}.npy"), mode="w+", dtype=np.int16, shape=oshape)
             pin_out = [torch.empty((N,) + oshape[1:], dtype=torch.int16).pin_memory() for _ in range(2)]
             done_out = [torch.cuda.Event(), torch.cuda.Event()]
+        elif cache_format:
+            out = QuantizedCache(torch, cache_format, cache_group, oshape, tdt, dev, host)
         elif host:
             out = torch.empty(oshape, dtype=tdt, pin_memory=True)
         else:
             out = torch.empty(oshape, dtype=tdt, device=dev)
-        in_dev = (not disk_in) and cur.is_cuda
+        coded_in = isinstance(cur, QuantizedCache)
+        in_dev = (not disk_in) and (not coded_in) and cur.is_cuda
         stage_in = None if in_dev else torch.empty((N,) + tuple(cur.shape[1:]), dtype=tdt, device=dev)
-        stage_out = [torch.empty((N,) + oshape[1:], dtype=tdt, device=dev) for _ in range(2)] if (host or disk) else None
+        stage_out = [torch.empty((N,) + oshape[1:], dtype=tdt, device=dev) for _ in range(2)] if (host or disk or cache_format) else None
+        stage_codes = [(torch.empty((N,) + oshape[1:], dtype=torch.uint8, device=dev), torch.empty((N, out.scales.shape[1]), device=dev))
+                       for _ in range(2)] if cache_format and host else None
         t1 = time.perf_counter()
         pending = []      # disk: (chunk start, count, buffer) whose device -> pinned copy is in flight
         for ci, s in enumerate(range(0, K, N)):
@@ -270,6 +314,9 @@ def train_blockwise(nf, torch, wl, data, labels, epochs=1, lr=0.01, seed=1, log=
             if disk_in:                   # the block's input set is a cache file: read the chunk, then bring it in
                 stage_in[:cnt].view(torch.int16).copy_(torch.from_numpy(np.ascontiguousarray(cur[s:s + cnt])))
                 src = stage_in[:cnt]
+            elif coded_in:                # ... or holds 8-bit codes
+                src = stage_in[:cnt]
+                cur.read(nf, None, torch.arange(s, s + cnt, dtype=torch.int32, device=dev), src, None)
             elif stage_in is not None:    # ... or lives in host memory
                 stage_in[:cnt].copy_(cur[s:s + cnt], non_blocking=True)
                 src = stage_in[:cnt]
@@ -285,6 +332,9 @@ def train_blockwise(nf, torch, wl, data, labels, epochs=1, lr=0.01, seed=1, log=
                 pin_out[b][:cnt].copy_(stage_out[b][:cnt].view(torch.int16), non_blocking=True)
                 done_out[b].record(main)
                 pending.append((s, cnt, b))
+            elif cache_format:            # forward into a device chunk, quantised into the cache (by way of the device where it is pinned)
+                block.cache(src, stage_out[ci % 2][:cnt], count=cnt)
+                out.write(nf, s, stage_out[ci % 2][:cnt], stage_codes[ci % 2] if host else None)
             elif host:                    # forward into a device chunk, then an asynchronous copy to the pinned cache
                 so = stage_out[ci % 2]
                 block.cache(src, so[:cnt], count=cnt)
@@ -292,6 +342,8 @@ def train_blockwise(nf, torch, wl, data, labels, epochs=1, lr=0.01, seed=1, log=
             else:
                 block.cache(src, out[s:s + cnt], count=cnt)
         torch.cuda.synchronize()
+        if cache_format and nf.nf_op_status():
+            raise RuntimeError(f"block {bi}: activations that are not finite cannot be cached in 8 bits")
         for s0, c0, b0 in pending:
             out[s0:s0 + c0] = pin_out[b0][:c0].numpy()
         if disk:
@@ -338,6 +390,7 @@ def main():
     ap.add_argument("--budget-gb", type=float, default=0.0, help="re-plan the blocks with the Profiler and Algorithm 1 under this memory budget")
     ap.add_argument("--rho", type=float, default=0.4)
     ap.add_argument("--cache", default="hbm", choices=["hbm", "host", "disk"], help="where the activation cache of a finished block lives")
+    ap.add_argument("--cache-format", default=None, choices=["int8", "e4m3"], help="hold the cache (hbm, host) in 8 bits")
     ap.add_argument("--spill-dir", default=None, help='directory of the cache files (--cache disk) and of the off-loaded blocks')
     ap.add_argument("--offload", action="store_true", help="write each finished block's parameters to <spill-dir>/block<i>.npz")
     ap.add_argument("--measured-profiler", action="store_true", help="with --budget-gb: profile by running steps instead of sizing buffers")
@@ -365,7 +418,7 @@ def main():
     t0 = time.perf_counter()
     res = train_blockwise(nf, torch, wl, data, labels, epochs=args.epochs, lr=args.lr, log=lambda r: print(json.dumps(r), flush=True),
                           val=val, cache=args.cache, spill_dir=args.spill_dir,
-                          offload=(args.spill_dir if args.offload else None))
+                          offload=(args.spill_dir if args.offload else None), cache_format=args.cache_format)
     wall = time.perf_counter() - t0
     if val:
         print(json.dumps(dict(exit_table=[(l, round(a, 4), p) for l, a, p in res[2]["table"]], selected_exit=res[2]["selected"])))
