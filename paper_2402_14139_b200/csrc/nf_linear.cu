@@ -83,14 +83,28 @@ __global__ void __launch_bounds__(256) gemm_simple_kernel(const float* __restric
     }
 }
 
-template <typename T>
+// The partial sums of an element in LN chains (chain k takes splits k, k + LN, ...) in fp64, joined in order: one chain where there are many
+// elements, eight threads to an element where there are few
+template <typename T, int LN>
 __global__ void __launch_bounds__(256) gemm_join_kernel(const float* __restrict__ part, int splits, size_t n, int Q, const Epilogue e) {
   nf_pdl_begin();
-  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= n) return;
+  constexpr int kCols = 256 / LN;
+  __shared__ double sm[LN][kCols];
+  const int tx = threadIdx.x % kCols, ty = threadIdx.x / kCols;
+  const size_t i = (size_t)blockIdx.x * kCols + tx;
   double s = 0;
-  for (int z = 0; z < splits; ++z) s += part[(size_t)z * n + i];
-  finish<T>(e, i, (int)(i % Q), (float)s);
+  if (i < n) {
+#pragma unroll 4
+    for (int z = ty; z < splits; z += LN) s += part[(size_t)z * n + i];
+  }
+  if constexpr (LN > 1) {
+    sm[ty][tx] = s;
+    __syncthreads();
+    if (ty) return;
+#pragma unroll
+    for (int k = 1; k < LN; ++k) s += sm[k][tx];
+  }
+  if (i < n) finish<T>(e, i, (int)(i % Q), (float)s);
 }
 
 // A few rows of x (MR at most) through weights contiguous along r: the weights are all the traffic.  A block of 128 threads takes kThinRows
@@ -161,6 +175,149 @@ template <typename T>
 int thin_product(const T* x, const T* w, int M, int N, int K, const Epilogue& e) {
   auto k = M == 1 ? thin_kernel<T, 1> : M == 2 ? thin_kernel<T, 2> : M <= 4 ? thin_kernel<T, 4> : thin_kernel<T, kThinMost<T>>;
   nf_launch(k, (unsigned)((N + kThinRows - 1) / kThinRows), 128, 0, x, w, M, N, K, e);
+  NF_LAUNCHED();
+  return NF_OK;
+}
+
+// Many rows times a small matrix (R and Q up to 64, kRowsMost in all: 1x1 convolutions of few channels), where narrow rows come slowly through TMA
+// (13 cycles each).  143962 x 16 x 56 bf16 24 us (29 on the tensor cores), 96631 x 45 x 30 fp32 27 us (147); at 64 x 64 the products bound it, 200704 rows
+// of bf16 128 us (32 there).  A block takes kRowTile rows, contiguous in memory, through shared memory in whole 16-byte pieces;
+// the matrix lies there as fp32 [r][q]; two threads per row compute half of its results each, pairs of neighbours in one packed multiply-add; the
+// results go through shared memory again, so that everything per result (residual, pre, y) is read and written in order.
+constexpr int kRowTile = 128, kRowsMost = 2048;
+
+template <typename T>
+struct RowShape {  // floats in shared memory: matrix, rows of A (an odd pitch: a warp reads one column of 32 rows), results
+  int Qp, pa, py;
+  __host__ __device__ RowShape(int R, int Q, int QH) : Qp(2 * QH), pa(R | 1), py(Q | 1) {}
+  __host__ __device__ size_t bytes(int R) const { return ((size_t)((R * Qp + kRowTile * pa + 3) & ~3) + (size_t)kRowTile * py) * 4; }
+};
+
+template <typename T, int QH>  // results per thread
+__global__ void __launch_bounds__(2 * kRowTile) rows_kernel(const T* __restrict__ A, const T* __restrict__ B, int P, int Q, int R, int b_along_r,
+                                                            const Epilogue e) {
+  nf_pdl_begin();
+  extern __shared__ __align__(16) float rsm[];
+  const RowShape<T> sh(R, Q, QH);
+  float* bs = rsm;
+  float* as = bs + R * sh.Qp;
+  float* ys = rsm + ((R * sh.Qp + kRowTile * sh.pa + 3) & ~3);
+  constexpr int NT = 2 * kRowTile;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < R * sh.Qp; i += NT) {
+    const int r = i / sh.Qp, q = i - r * sh.Qp;
+    bs[i] = q < Q ? ldf(B, b_along_r ? (size_t)q * R + r : (size_t)r * Q + q) : 0.f;
+  }
+  const int p0 = blockIdx.x * kRowTile, rows = min(kRowTile, P - p0), na = rows * R;
+  const T* from = A + (size_t)p0 * R;  // a multiple of 16 bytes from the start
+#pragma unroll 2
+  for (int i = threadIdx.x * 8; i < na; i += NT * 8) {
+    float v[8];
+    if (i + 8 <= na) {
+      ld8(from + i, v);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = i + j < na ? ldf(from, i + j) : 0.f;
+    }
+    int row = i / R, c = i - row * R;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (i + j < na) as[row * sh.pa + c] = v[j];
+      if (++c == R) {
+        c = 0;
+        ++row;
+      }
+    }
+  }
+  __syncthreads();
+  const int half = threadIdx.x / kRowTile, row = threadIdx.x % kRowTile;
+  if (row < rows) {
+    f32x2 acc[QH / 2];
+#pragma unroll
+    for (int i = 0; i < QH / 2; ++i) acc[i] = 0;
+    const float* a = as + row * sh.pa;
+    const float* b = bs + half * QH;
+#pragma unroll 4
+    for (int r = 0; r < R; ++r, b += sh.Qp) {
+      const f32x2 aa = nf_pack2(a[r], a[r]);
+#pragma unroll
+      for (int i = 0; i < QH / 4; ++i) {
+        const float4 w = *reinterpret_cast<const float4*>(b + 4 * i);
+        acc[2 * i] = nf_fma2(aa, nf_pack2(w.x, w.y), acc[2 * i]);
+        acc[2 * i + 1] = nf_fma2(aa, nf_pack2(w.z, w.w), acc[2 * i + 1]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < QH / 2; ++i) {
+      float lo, hi;
+      nf_unpack2(acc[i], lo, hi);
+      const int q = half * QH + 2 * i;
+      if (q < Q) ys[row * sh.py + q] = lo;
+      if (q + 1 < Q) ys[row * sh.py + q + 1] = hi;
+    }
+  }
+  __syncthreads();
+  const int ny = rows * Q;
+  const size_t at0 = (size_t)p0 * Q;
+  for (int i = threadIdx.x * 8; i < ny; i += NT * 8) {  // eight results in a row of memory
+    float v[8];
+    int r = i / Q, q = i - r * Q;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      v[j] = i + j < ny ? ys[r * sh.py + q] + (e.bias ? e.bias[q] : 0.f) : 0.f;
+      if (++q == Q) {
+        q = 0;
+        ++r;
+      }
+    }
+    if (i + 8 <= ny) {
+      if (e.residual) {
+        float s[8];
+        ld8(reinterpret_cast<const T*>(e.residual) + at0 + i, s);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += s[j];
+      }
+      if (e.pre) {
+        float s[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] = v[j];
+        st8(reinterpret_cast<T*>(e.pre) + at0 + i, s);
+      }
+      if (e.act != NF_ACT_NONE) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = nf_act_value<T>(v[j], e.act);
+      }
+      st8(reinterpret_cast<T*>(e.out) + at0 + i, v);
+    } else {
+      for (int j = 0; j < 8 && i + j < ny; ++j) {
+        float t = v[0];
+#pragma unroll
+        for (int k = 1; k < 8; ++k) t = j == k ? v[k] : t;
+        if (e.residual) t += ldf(reinterpret_cast<const T*>(e.residual), at0 + i + j);
+        if (e.pre) stf(reinterpret_cast<T*>(e.pre), at0 + i + j, t);
+        stf(reinterpret_cast<T*>(e.out), at0 + i + j, nf_act_value<T>(t, e.act));
+      }
+    }
+  }
+}
+
+template <typename T>
+int rows_product(const T* A, const T* B, int P, int Q, int R, bool b_along_r, const Epilogue& e) {
+  const int QH = Q <= 16 ? 8 : Q <= 32 ? 16 : 32;
+  auto k = QH == 8 ? rows_kernel<T, 8> : QH == 16 ? rows_kernel<T, 16> : rows_kernel<T, 32>;
+  const size_t smem = RowShape<T>(R, Q, QH).bytes(R);
+  static bool ready[64];
+  int dev = 0;
+  NF_CUDA(cudaGetDevice(&dev));
+  if (dev < 0 || dev >= 64) return NF_EUNSUPPORTED;
+  if (!ready[dev]) {
+    const int most = (int)RowShape<T>(64, 64, 32).bytes(64);
+    NF_CUDA(cudaFuncSetAttribute(rows_kernel<T, 8>, cudaFuncAttributeMaxDynamicSharedMemorySize, most));
+    NF_CUDA(cudaFuncSetAttribute(rows_kernel<T, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, most));
+    NF_CUDA(cudaFuncSetAttribute(rows_kernel<T, 32>, cudaFuncAttributeMaxDynamicSharedMemorySize, most));
+    ready[dev] = true;
+  }
+  nf_launch(k, (unsigned)((P + kRowTile - 1) / kRowTile), 2 * kRowTile, smem, A, B, P, Q, R, (int)b_along_r, e);
   NF_LAUNCHED();
   return NF_OK;
 }
@@ -264,7 +421,10 @@ struct Product {
 
 // bf16: always (a 128 x 64 x 10 product took 6 us there and 10 us on the CUDA cores).  fp32: from 2^26 multiply-adds on, where what
 // cutting the operands into parts costs is earned back (256 x 256 x 256 16 us there, 9 us here; 512 x 512 x 512 17 us and 24 us).
-bool on_tensor_cores(int dtype, const Product& d) { return dtype == NF_BF16 || (double)d.P * d.Q * d.R >= 67108864.0; }
+// Thin products stay off: their traffic, three parts written and read, costs more than the sums.
+bool on_tensor_cores(int dtype, const Product& d) {
+  return dtype == NF_BF16 || ((double)d.P * d.Q * d.R >= 67108864.0 && d.P >= 64 && d.Q >= 64 && d.R >= 64);
+}
 bool needs_copy(int dtype, int len) { return dtype == NF_F32 || len % 8; }
 size_t copy_bytes(int dtype, int rows, int len) {
   return needs_copy(dtype, len) ? nf_align_up((size_t)rows * pad8(len) * 2 * (dtype == NF_F32 ? 3 : 1), 256) : 0;
@@ -273,7 +433,7 @@ size_t copy_bytes(int dtype, int rows, int len) {
 int simple_splits(int P, int Q, int R) {
   const long tiles = (long)((P + 63) / 64) * ((Q + 63) / 64);
   long s = 296 / tiles;
-  if (s > R / 64) s = R / 64;  // four steps of 16 at least
+  if (s > R / 128) s = R / 128;  // eight steps of 16 at least
   return s < 1 ? 1 : (int)s;
 }
 
@@ -288,7 +448,10 @@ size_t product_bytes(int dtype, const Product& d) {
 template <typename T>
 int join(const float* part, int splits, int P, int Q, const Epilogue& e) {
   const size_t n = (size_t)P * Q;
-  nf_launch(gemm_join_kernel<T>, (unsigned)((n + 255) / 256), 256, 0, part, splits, n, Q, e);
+  if (n < 148 * 1024 && splits > 4)
+    nf_launch(gemm_join_kernel<T, 8>, (unsigned)((n + 31) / 32), 256, 0, part, splits, n, Q, e);
+  else
+    nf_launch(gemm_join_kernel<T, 1>, (unsigned)((n + 255) / 256), 256, 0, part, splits, n, Q, e);
   NF_LAUNCHED();
   return NF_OK;
 }
@@ -321,6 +484,7 @@ template <typename T>
 int product(const Product& d, const void* A, const void* B, void* scratch, const Epilogue& e) {
   const int dtype = sizeof(T) == 4 ? NF_F32 : NF_BF16;
   if ((d.Q + 63) / 64 > 65535) return NF_EUNSUPPORTED;
+  if (d.a_along_r && d.R <= 64 && d.Q <= 64 && d.R * d.Q <= kRowsMost) return rows_product<T>((const T*)A, (const T*)B, d.P, d.Q, d.R, d.b_along_r, e);
   if (d.P <= kThinMost<T> && d.a_along_r && d.b_along_r && d.R % (16 / (int)sizeof(T)) == 0)
     return thin_product<T>((const T*)A, (const T*)B, d.P, d.Q, d.R, e);
   if constexpr (sizeof(T) == 4) {

@@ -67,6 +67,27 @@ template <> struct Raw<float, 4> {
   }
   __device__ __forceinline__ f32x2 pair(int i) const { return i == 0 ? nf_pack2(u.x, u.y) : nf_pack2(u.z, u.w); }
 };
+template <> struct Raw<bf16, 4> {
+  uint2 u;
+  __device__ __forceinline__ void load(const bf16* p) { u = *reinterpret_cast<const uint2*>(p); }
+  __device__ __forceinline__ void load_last(const bf16* p) { u = __ldcs(reinterpret_cast<const uint2*>(p)); }
+  __device__ __forceinline__ f32x2 pair(int i) const {
+    const uint32_t w = i == 0 ? u.x : u.y;
+    return nf_pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+  }
+};
+template <> struct Raw<bf16, 2> {
+  uint32_t u;
+  __device__ __forceinline__ void load(const bf16* p) { u = *reinterpret_cast<const uint32_t*>(p); }
+  __device__ __forceinline__ void load_last(const bf16* p) { u = __ldcs(reinterpret_cast<const uint32_t*>(p)); }
+  __device__ __forceinline__ f32x2 pair(int) const { return nf_pack2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u)); }
+};
+template <> struct Raw<float, 2> {
+  float2 u;
+  __device__ __forceinline__ void load(const float* p) { u = *reinterpret_cast<const float2*>(p); }
+  __device__ __forceinline__ void load_last(const float* p) { u = __ldcs(reinterpret_cast<const float2*>(p)); }
+  __device__ __forceinline__ f32x2 pair(int) const { return nf_pack2(u.x, u.y); }
+};
 template <typename T> struct Raw<T, 1> {
   float u;
   __device__ __forceinline__ void load(const T* p) { u = ldf(p, 0); }
@@ -78,14 +99,18 @@ __device__ __forceinline__ void store(T* p, const f32x2 (&v)[(V + 1) / 2]) {
   float f[V + 1];
 #pragma unroll
   for (int i = 0; i < (V + 1) / 2; ++i) nf_unpack2(v[i], f[2 * i], f[2 * i + 1]);
-  if constexpr (V == 8) {
-    uint32_t w[4];
+  if constexpr (V > 1 && sizeof(T) == 2) {
+    uint32_t w[V / 2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < V / 2; ++i) {
       const __nv_bfloat162 b = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
       w[i] = *reinterpret_cast<const uint32_t*>(&b);
     }
-    __stcs(reinterpret_cast<uint4*>(p), make_uint4(w[0], w[1], w[2], w[3]));
+    if constexpr (V == 8) __stcs(reinterpret_cast<uint4*>(p), make_uint4(w[0], w[1], w[2], w[3]));
+    else if constexpr (V == 4) __stcs(reinterpret_cast<uint2*>(p), make_uint2(w[0], w[1]));
+    else __stcs(reinterpret_cast<uint32_t*>(p), w[0]);
+  } else if constexpr (V == 2) {
+    __stcs(reinterpret_cast<float2*>(p), make_float2(f[0], f[1]));
   } else if constexpr (V == 4) {
     __stcs(reinterpret_cast<float4*>(p), make_float4(f[0], f[1], f[2], f[3]));
   } else {
@@ -161,9 +186,9 @@ struct Chan {
 // ---------------------------------------------------------------- large images
 // V channels per thread; threads run along the channels of a pixel first, then along the pixels
 template <typename T, int V, int ACT, bool BWD>
-__global__ void __launch_bounds__(kNT, 2) group_norm_kernel(const GnArgs a) {
+__global__ void __launch_bounds__(kNT, V == 8 ? 2 : 4) group_norm_kernel(const GnArgs a) {
   nf_pdl_begin();
-  constexpr int NP = (V + 1) / 2, U = BWD ? 4 : 8;  // loads in flight per thread and tensor
+  constexpr int NP = (V + 1) / 2, U = V < 8 || BWD ? 4 : 8;  // loads in flight per thread and tensor
   extern __shared__ __align__(16) float sm[];
   float* red = sm;                        // [2V][kNT] tree reduction
   float* tot = red + 2 * V * kNT;         // [2][2][Cs] this block's channel sums, two images in turn
@@ -353,7 +378,7 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_kernel(const GnArgs a) {
         }
         store<T, V>(to, o);
       };
-      constexpr int W = BWD ? 4 : 8;
+      constexpr int W = V < 8 || BWD ? 4 : 8;
       int p = p0 + tr;
       const size_t step = (size_t)R * a.C;
       size_t at = col + (size_t)p * a.C;
@@ -910,10 +935,10 @@ GnPlan plan_gn(int dtype, int N, int P, int C, int groups, bool bwd) {
   const size_t es = nf_esize(dtype);
   if (plan_held(N, P, C, cpg, 16 / (int)es, bwd, &pl)) return pl;
   const size_t image = (size_t)P * C * es * (bwd ? 2 : 1);
-  // 16 bytes per thread where the slices allow it, else single channels.  A slice is some whole groups: all of them, fewer where C is
+  // 16 bytes per thread where the slices allow it, else fewer, down to single channels.  A slice is some whole groups: all of them, fewer where C is
   // above kMaxCs, where one image per (largest portable) cluster would leave most SMs idle, or where the images in work (two blocks
   // on each SM) would fill half of L2 -- but not below 64 bytes of a pixel.
-  for (pl.V = 16 / (int)es;; pl.V = 1) {
+  for (pl.V = 16 / (int)es;; pl.V /= 2) {
     pl.slices = 0;
     for (int s = 1; s <= groups; ++s) {
       if (groups % s || C / s > kMaxCs || C / s % pl.V) continue;
@@ -974,7 +999,7 @@ int launch_gn(GnArgs& a, GnPlan& pl) {
   auto k = group_norm_kernel<T, V, ACT, BWD>;
   if (!ready[dev]) {
     int rc = allow(k, 200 * 1024);
-    if constexpr (V > 1) {
+    if constexpr (V * sizeof(T) == 16) {
       if (rc == NF_OK) rc = allow(group_norm_held_kernel<T, V, ACT, BWD, true, 256, false>, kHeldBytes);
       if (rc == NF_OK) rc = allow(group_norm_held_kernel<T, V, ACT, BWD, false, 256, false>, kHeldBytes);
       if (rc == NF_OK) rc = allow(group_norm_held_kernel<T, V, ACT, BWD, true, 512, true>, 2 * kHeldBytes);
@@ -983,7 +1008,7 @@ int launch_gn(GnArgs& a, GnPlan& pl) {
     if (rc != NF_OK) return rc;
     ready[dev] = true;
   }
-  if constexpr (V > 1) {
+  if constexpr (V * sizeof(T) == 16) {
     if (pl.TS) {
       const bool fine = a.cpg < V;
       auto held = fine ? (pl.threads == 512 ? group_norm_held_kernel<T, V, ACT, BWD, true, 512, true> : group_norm_held_kernel<T, V, ACT, BWD, true, 256, false>)
@@ -1013,11 +1038,17 @@ int launch_gn(GnArgs& a, GnPlan& pl) {
   return NF_OK;
 }
 
-// bf16 has a kernel per activation; fp32 and odd channel counts ask at run time
+// bf16 has a kernel per activation; fp32 and channel counts that are no multiple of eight ask at run time
 template <bool BWD>
 int run_gn(int dtype, GnArgs& a, GnPlan& pl) {
-  if (dtype == NF_F32) return pl.V == 4 ? launch_gn<float, 4, kAnyAct, BWD>(a, pl) : launch_gn<float, 1, kAnyAct, BWD>(a, pl);
-  if (pl.V == 1) return launch_gn<bf16, 1, kAnyAct, BWD>(a, pl);
+  if (dtype == NF_F32)
+    return pl.V == 4   ? launch_gn<float, 4, kAnyAct, BWD>(a, pl)
+           : pl.V == 2 ? launch_gn<float, 2, kAnyAct, BWD>(a, pl)
+                       : launch_gn<float, 1, kAnyAct, BWD>(a, pl);
+  if (pl.V < 8)
+    return pl.V == 4   ? launch_gn<bf16, 4, kAnyAct, BWD>(a, pl)
+           : pl.V == 2 ? launch_gn<bf16, 2, kAnyAct, BWD>(a, pl)
+                       : launch_gn<bf16, 1, kAnyAct, BWD>(a, pl);
   switch (a.act) {
     case NF_ACT_NONE: return launch_gn<bf16, 8, NF_ACT_NONE, BWD>(a, pl);
     case NF_ACT_RELU: return launch_gn<bf16, 8, NF_ACT_RELU, BWD>(a, pl);
