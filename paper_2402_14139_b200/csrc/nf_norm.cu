@@ -6,12 +6,14 @@
 //
 // HBM has to carry every tensor once; the two passes over an image that the formulas need have to find it on the chip.  Two forms:
 //  - where a pixel of the slice (some whole groups) is a power of two of 16-byte pieces: teams of a warp up to clusters of sixteen blocks hold a
-//    slice in shared memory, and fill each place anew as soon as the second pass has read it, so that copies run under both passes.
+//    slice, or as much of it as fits, in shared memory, and fill each place anew as soon as the second pass has read it, so that copies run under
+//    both passes; the rest passes through a small ring of places, from HBM and then from L2.
 //  - any other shape: a cluster of blocks reads its slice twice, the second time from L2.
 // Parameter gradients gather in registers or shared memory over all images of a team or block, then in one row of partials each.
 //
-// Sums: a thread adds in fp32 what it sees of its channels, in the forward pass after subtracting a value of the group or channel, so that a mean far from zero costs no digits; ranges of pixels are joined by their means and squared deviations.  For ReLU
-// xh and z are formed by separately rounded operations in this order in both directions, so that the gradient's mask is the forward's.
+// Sums: a thread adds in fp32 what it sees of its channels, in the forward pass after subtracting a value of the group or channel, so that a
+// mean far from zero costs no digits; ranges of pixels are joined by their means and squared deviations.  The gradient's ReLU mask is
+// decided on xh gamma + beta with every operation rounded by itself.
 #include <cooperative_groups.h>
 
 #include <cuda.h>
@@ -123,30 +125,50 @@ __device__ __forceinline__ float high(f32x2 v) { float a, b; nf_unpack2(v, a, b)
 
 // ACT: an nf_act known to the compiler, or kAnyAct: `act` says
 constexpr int kAnyAct = -1;
+// Two sigmoids; in bf16 storage as nf_sigmoid, its scaling and sum taken in pairs
+template <typename T>
+__device__ __forceinline__ f32x2 sigmoid2(f32x2 z) {
+  float a, b;
+  if constexpr (std::is_same<T, float>::value) {
+    nf_unpack2(z, a, b);
+    return nf_pack2(nf_sigmoid<T>(a), nf_sigmoid<T>(b));
+  }
+  nf_unpack2(nf_mul2(z, both(-1.4426950408889634f)), a, b);
+  asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(a));
+  asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(b));
+  nf_unpack2(nf_add2(nf_pack2(a, b), both(1.f)), a, b);
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(a));
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(b));
+  return nf_pack2(a, b);
+}
 template <typename T, int ACT>
 __device__ __forceinline__ f32x2 act2(f32x2 z, int act) {
   if constexpr (ACT == NF_ACT_NONE) return z;
+  if constexpr (ACT == NF_ACT_SILU) return nf_mul2(z, sigmoid2<T>(z));
   float a, b;
   nf_unpack2(z, a, b);
   return nf_pack2(nf_act_value<T>(a, ACT == kAnyAct ? act : ACT), nf_act_value<T>(b, ACT == kAnyAct ? act : ACT));
 }
-// dz = dy act'(z)
+// dz = dy act'(z), z = xh ga + be.  ReLU: z > 0 is decided as the product, rounded by itself, being above -be; the sum of the two, rounded,
+// has the sign of the exact one.
 template <typename T, int ACT>
-__device__ __forceinline__ f32x2 grad2(f32x2 z, f32x2 dy, int act) {
+__device__ __forceinline__ f32x2 grad2(f32x2 xh, f32x2 ga, f32x2 be, f32x2 dy, int act) {
   if constexpr (ACT == NF_ACT_NONE) return dy;
-  float a, b;
-  nf_unpack2(z, a, b);
+  float a, b, c, d;
   if constexpr (ACT == NF_ACT_RELU) {
-    float c, d;
+    float e, f;
+    nf_unpack2(nf_mul2(xh, ga), a, b);
+    nf_unpack2(be, e, f);
     nf_unpack2(dy, c, d);
-    return nf_pack2(a > 0.f ? c : 0.f, b > 0.f ? d : 0.f);
+    return nf_pack2(a > -e ? c : 0.f, b > -f ? d : 0.f);
   }
   if constexpr (ACT == NF_ACT_SILU) {  // s (1 + z (1 - s))
-    const f32x2 s = nf_pack2(nf_sigmoid<T>(a), nf_sigmoid<T>(b));
+    const f32x2 z = nf_fma2(xh, ga, be), s = sigmoid2<T>(z);
     const f32x2 t = nf_fma2(nf_mul2(z, s), nf_fma2(s, both(-1.f), both(1.f)), s);
     return nf_mul2(t, dy);
   }
-  float c, d;
+  const f32x2 z = ACT == kAnyAct ? nf_add_each(nf_mul2(xh, ga), be) : nf_fma2(xh, ga, be);
+  nf_unpack2(z, a, b);
   nf_unpack2(dy, c, d);
   return nf_pack2(nf_act_dz<T>(a, c, ACT == kAnyAct ? act : ACT), nf_act_dz<T>(b, d, ACT == kAnyAct ? act : ACT));
 }
@@ -175,11 +197,11 @@ struct Chan {
   }
   __device__ __forceinline__ f32x2 scale(int i) const { return rs[ONE ? 0 : i]; }
   __device__ __forceinline__ f32x2 xh(f32x2 x, int i) const { return nf_mul2(nf_add2(x, nmu[ONE ? 0 : i]), rs[ONE ? 0 : i]); }
-  // ReLU, whose gradient is a decision on the sign: product and sum rounded one by one in both directions; else in one
-  template <int ACT>
-  __device__ __forceinline__ f32x2 z(f32x2 xh, int i) const {
-    if constexpr (ACT == NF_ACT_RELU || ACT == kAnyAct) return nf_add_each(nf_mul2(xh, ga[i]), be[i]);
-    return nf_fma2(xh, ga[i], be[i]);
+  // Forward: z from x as one sum and one multiply-add, the factor of a channel being gamma rstd
+  __device__ __forceinline__ f32x2 z(f32x2 x, const f32x2 (&factor)[NP], int i) const { return nf_fma2(nf_add2(x, nmu[ONE ? 0 : i]), factor[i], be[i]); }
+  __device__ __forceinline__ void factors(f32x2 (&factor)[NP]) const {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) factor[i] = nf_mul2(ga[i], rs[ONE ? 0 : i]);
   }
 };
 
@@ -239,7 +261,7 @@ __global__ void __launch_bounds__(kNT, V == 8 ? 2 : 4) group_norm_kernel(const G
           for (int i = 0; i < NP; ++i) {
             if constexpr (BWD) {
               const f32x2 xh = ch.xh(v.pair(i), i);
-              const f32x2 dz = grad2<T, ACT>(ACT == NF_ACT_NONE ? xh : ch.template z<ACT>(xh, i), g.pair(i), a.act);
+              const f32x2 dz = grad2<T, ACT>(xh, ch.ga[i], ch.be[i], g.pair(i), a.act);
               s[i] = nf_add2(s[i], dz);
               q[i] = nf_fma2(dz, xh, q[i]);
             } else {
@@ -364,16 +386,18 @@ __global__ void __launch_bounds__(kNT, V == 8 ? 2 : 4) group_norm_kernel(const G
           m2[i] = nf_pack2(-gsm[gps + g], -gsm[gps + h]);
         }
       }
+      f32x2 factor[NP];
+      if constexpr (!BWD) ch.factors(factor);
       auto result = [&](const Raw<T, V>& v, const Raw<T, V>& g, T* to) {
         f32x2 o[NP];
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-          const f32x2 xh = ch.xh(v.pair(i), i);
           if constexpr (BWD) {
-            const f32x2 dz = grad2<T, ACT>(ACT == NF_ACT_NONE ? xh : ch.template z<ACT>(xh, i), g.pair(i), a.act);
+            const f32x2 xh = ch.xh(v.pair(i), i);
+            const f32x2 dz = grad2<T, ACT>(xh, ch.ga[i], ch.be[i], g.pair(i), a.act);
             o[i] = nf_mul2(ch.scale(i), nf_fma2(xh, m2[i], nf_fma2(ch.ga[i], dz, m1[i])));
           } else {
-            o[i] = act2<T, ACT>(ch.template z<ACT>(xh, i), a.act);
+            o[i] = act2<T, ACT>(ch.z(v.pair(i), factor, i), a.act);
           }
         }
         store<T, V>(to, o);
@@ -432,9 +456,13 @@ __device__ __forceinline__ void copies_wait(int behind) {  // all but the latest
   else asm volatile("cp.async.wait_group 3;" ::: "memory");
 }
 
-template <typename T, int V, int ACT, bool BWD, bool FINE, int NT, bool MORE>
-__global__ void __launch_bounds__(NT, 512 / NT) group_norm_held_kernel(const GnArgs a) {
-  constexpr int NP = V / 2, S = FINE ? V : 1, kTensors = BWD ? 2 : 1;
+// Places per thread and tensor that the rest of a large image passes through: 32 KB on their way in a block, two blocks on an SM.  64 images of
+// 224x224x64 forward: 4 places 222 us, 6 and more 208 to 212.
+__host__ __device__ constexpr int held_ring(bool bwd) { return bwd ? 4 : 8; }
+
+template <typename T, int V, int ACT, bool BWD, bool FINE, bool MORE>
+__global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a) {
+  constexpr int NT = kNT, NP = V / 2, S = FINE ? V : 1, kTensors = BWD ? 2 : 1, kRing = held_ring(BWD);
   extern __shared__ __align__(16) uint8_t held_raw[];
   __shared__ float part[NT / 32][2][kSlotGroups];        // per warp: totals of the slots (groups, or FINE channels)
   __shared__ float2 gsm[NT / 32 * 32];                  // per team: mean and rstd, or m1 and m2
@@ -448,9 +476,10 @@ __global__ void __launch_bounds__(NT, 512 / NT) group_norm_held_kernel(const GnA
   const int lo = a.cpg > V ? a.cpg / V : 1;
   const int p0 = rank * a.rpc, np = max(0, min(a.P - p0, a.rpc));
   // Turns over the slice: `whole` of them with a piece for every thread, then one where some have none.  The first a.hold are held; the rest of
-  // a very large image (MORE) is read again, from L2.
+  // a very large image (MORE), ks pieces of this thread, passes through a ring of kRing places twice, the second time from L2.
   const int whole = np * a.vpr / TS, kw = min(whole, a.hold);
   const bool last = t < np * a.vpr - whole * TS, last_held = last && whole < a.hold;
+  const int ks = MORE ? whole - kw + (last && !last_held) : 0;
   if (a.CS > 1) {
     if (threadIdx.x == 0) {
       ptx::mbar_init(&xbar[0], 1);
@@ -481,6 +510,64 @@ __global__ void __launch_bounds__(NT, 512 / NT) group_norm_held_kernel(const GnA
       }
     }
     copies_end();
+  }
+  // The ring's loads run kRing pieces ahead of their use, through both passes and from one image to the next: (image, pass, pieces left, where)
+  const uint32_t ring0 = slot0 + kTensors * a.hold * kstep;
+  const size_t ring_at = (size_t)tr * a.C + a.hold * row_step;
+  int ring_n = first, ring_left = ks;
+  bool ring_second = false;
+  uint32_t ring_slot = 0;  // place of the next piece to be used
+  const T* ring_x = x + (size_t)first * image + ring_at;
+  const T* ring_dy = BWD ? dy + (size_t)first * image + ring_at : nullptr;
+  auto ring_fill = [&](uint32_t place) {
+    if (ring_n < a.N && ks) {
+      copy16(ring0 + place * kstep, ring_x);
+      ring_x += row_step;
+      if constexpr (BWD) {
+        copy16(ring0 + (kRing + place) * kstep, ring_dy);
+        ring_dy += row_step;
+      }
+      if (--ring_left == 0) {
+        ring_left = ks;
+        if (ring_second) ring_n += a.stride;
+        ring_second = !ring_second;
+        ring_x = x + (size_t)ring_n * image + ring_at;
+        if constexpr (BWD) ring_dy = dy + (size_t)ring_n * image + ring_at;
+      }
+    }
+    copies_end();
+  };
+  auto ring_use = [&](auto&& f) {  // f(x, dy) for each of this pass's pieces
+    auto step = [&](auto&& fill) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
+      Raw<T, V> v, g;
+      v.load_shared(ring0 + ring_slot * kstep);
+      if constexpr (BWD) g.load_shared(ring0 + (kRing + ring_slot) * kstep);
+      else g = v;
+      f(v, g);
+      fill();  // the piece has been read: what became of it depends on it
+      ring_slot = (ring_slot + 1) % kRing;
+    };
+    auto along = [&] {  // within a pass the loads move on by rows
+      copy16(ring0 + ring_slot * kstep, ring_x);
+      ring_x += row_step;
+      if constexpr (BWD) {
+        copy16(ring0 + (kRing + ring_slot) * kstep, ring_dy);
+        ring_dy += row_step;
+      }
+      copies_end();
+    };
+    const int same = ks - kRing;  // steps whose loads belong to this pass as well; the last of them is the pass's last load
+    int k = 0;
+    if (same > 1 && ring_n < a.N) {
+#pragma unroll 4
+      for (; k < same - 1; ++k) step(along);
+      ring_left -= same - 1;
+    }
+    for (; k < ks; ++k) step([&] { ring_fill(ring_slot); });
+  };
+  if (MORE && ks) {
+    for (uint32_t i = 0; i < kRing; ++i) ring_fill(i);
   }
   Chan<V, !FINE> ch;
   constexpr int NS = FINE ? NP : 1;
@@ -532,7 +619,7 @@ __global__ void __launch_bounds__(NT, 512 / NT) group_norm_held_kernel(const GnA
       for (int i = 0; i < NP; ++i) {
         if constexpr (BWD) {
           const f32x2 xh = ch.xh(v.pair(i), i);
-          const f32x2 dz = grad2<T, ACT>(ACT == NF_ACT_NONE ? xh : ch.template z<ACT>(xh, i), g.pair(i), a.act);
+          const f32x2 dz = grad2<T, ACT>(xh, ch.ga[i], ch.be[i], g.pair(i), a.act);
           s[i] = nf_add2(s[i], dz);
           q[i] = nf_fma2(dz, xh, q[i]);
         } else {
@@ -543,29 +630,12 @@ __global__ void __launch_bounds__(NT, 512 / NT) group_norm_held_kernel(const GnA
       }
     };
     const size_t own_at = (size_t)n * image + (size_t)tr * a.C;  // this thread's first piece
-    constexpr int U = BWD ? 2 : 4;  // pieces of a very large image in flight per thread and tensor
-    if constexpr (MORE) {
-      size_t at = own_at + a.hold * row_step;
-      int left = whole - a.hold;
-      for (; left >= U; left -= U) {
-        Raw<T, V> v[U], g[BWD ? U : 1];
-#pragma unroll
-        for (int u = 0; u < U; ++u, at += row_step) {
-          v[u].load(x + at);
-          if constexpr (BWD) g[u].load(dy + at);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) add(v[u], g[BWD ? u : 0]);
-      }
-      for (left += last; left > 0; --left, at += row_step) {
-        Raw<T, V> v, g;
-        v.load(x + at);
-        if constexpr (BWD) g.load(dy + at);
-        else g = v;
-        add(v, g);
-      }
+    if constexpr (MORE) {  // what is held was asked for before the latest kRing pieces of the ring, unless the image hardly needs it
+      if (ks >= kRing) asm volatile("cp.async.wait_group %0;" ::"n"(kRing) : "memory");
+      else copies_wait(ks ? 0 : a.buffers - 1);
+    } else {
+      copies_wait(a.buffers - 1);
     }
-    copies_wait(a.buffers - 1);
     {
       auto one = [&](uint32_t at) {
         Raw<T, V> v, g;
@@ -582,6 +652,7 @@ __global__ void __launch_bounds__(NT, 512 / NT) group_norm_held_kernel(const GnA
       }
       for (k += last_held; k > 0; --k, at += kstep) one(at);
     }
+    if constexpr (MORE) ring_use(add);
     if constexpr (BWD) {
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
@@ -731,16 +802,18 @@ __global__ void __launch_bounds__(NT, 512 / NT) group_norm_held_kernel(const GnA
         ch.rs[i] = nf_pack2(g.y, h.y);
       }
     }
+    f32x2 factor[NP];
+    if constexpr (!BWD) ch.factors(factor);
     auto result = [&](const Raw<T, V>& v, const Raw<T, V>& g, T* to) {
       f32x2 o[NP];
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
-        const f32x2 xh = ch.xh(v.pair(i), i);
         if constexpr (BWD) {
-          const f32x2 dz = grad2<T, ACT>(ACT == NF_ACT_NONE ? xh : ch.template z<ACT>(xh, i), g.pair(i), a.act);
+          const f32x2 xh = ch.xh(v.pair(i), i);
+          const f32x2 dz = grad2<T, ACT>(xh, ch.ga[i], ch.be[i], g.pair(i), a.act);
           o[i] = nf_mul2(ch.scale(i), nf_fma2(xh, m2[FINE ? i : 0], nf_fma2(ch.ga[i], dz, m1[FINE ? i : 0])));
         } else {
-          o[i] = act2<T, ACT>(ch.template z<ACT>(xh, i), a.act);
+          o[i] = act2<T, ACT>(ch.z(v.pair(i), factor, i), a.act);
         }
       }
       store<T, V>(to, o);
@@ -778,29 +851,14 @@ __global__ void __launch_bounds__(NT, 512 / NT) group_norm_held_kernel(const GnA
     };
     if (n + a.buffers * a.stride < a.N) held(std::true_type());
     else held(std::false_type());
-    if constexpr (MORE) {
-      size_t at = own_at + a.hold * row_step;
-      int left = whole - a.hold;
-      for (; left >= U; left -= U) {
-        Raw<T, V> v[U], g[BWD ? U : 1];
-        size_t from = at;
-#pragma unroll
-        for (int u = 0; u < U; ++u, from += row_step) {
-          v[u].load_last(x + from);
-          if constexpr (BWD) g[u].load_last(dy + from);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u, at += row_step) result(v[u], g[BWD ? u : 0], out + at);
-      }
-      for (left += last; left > 0; --left, at += row_step) {
-        Raw<T, V> v, g;
-        v.load_last(x + at);
-        if constexpr (BWD) g.load_last(dy + at);
-        else g = v;
-        result(v, g, out + at);
-      }
-    }
     copies_end();
+    if constexpr (MORE) {
+      T* to = out + own_at + a.hold * row_step;
+      ring_use([&](const Raw<T, V>& v, const Raw<T, V>& g) {
+        result(v, g, to);
+        to += row_step;
+      });
+    }
     if (++b == a.buffers) b = 0;
     turn ^= 1;
   }
@@ -858,7 +916,8 @@ __global__ void __launch_bounds__(1024) group_norm_param_kernel(const float* __r
 
 struct GnPlan {
   int V, slices, CS, blocks, rows, stride;
-  int TS, threads, rpc, hold, buffers;  // held form: TS > 0
+  int TS, rpc, hold, buffers;  // held form: TS > 0
+  bool more;                   // it holds a part only
   size_t smem;
 };
 
@@ -872,61 +931,55 @@ bool slice_lanes(int C, int cpg, int full, int* least, int* most) {
   return true;
 }
 
-constexpr int kHeldBytes = 92 * 1024;  // of shared memory for two blocks of 256 threads on an SM; one of 512 has twice that
+constexpr int kHeldBytes = 92 * 1024;  // of shared memory per block, two on an SM
 
 // The held form.  Slices are 128 bytes of a pixel at least, where it has that many: at 64 the backward pass of 1904 images of 16x16x256 took 188 us,
-// at 128 145; at 32 the forward pass of 64 images of 224x224x64 608 us for 260 (other blocks read the rest of a line at other times).  Small images: the smallest
-// team (a warp to 256 threads) that holds a slice in kPer pieces a thread, the slice as wide as that allows.  Larger ones: blocks of 256
-// threads, two on an SM, or one of 512, in clusters that grow until the slice fits, or until there is work for the SMs; what sixteen blocks cannot
-// hold is read twice.
+// at 128 145; at 32 the forward pass of 64 images of 224x224x64 608 us for 260 (other blocks read the rest of a line at other times).  Small
+// images: the smallest team (a warp to a block) that holds a slice in kPer pieces a thread, the slice as wide as that allows.  Larger ones: a
+// block, or as few blocks as give the SMs work, since blocks that exchange sums wait for one another (512 images of 28x28x128 forward: one
+// block 53 us, two 61, four 103, eight 190), even where the slice then does not fit; 64 images of 224x224x64: two 222 us, four 213, eight 209.
 bool plan_held(int N, int P, int C, int cpg, int full, bool bwd, GnPlan* pl) {
   int least, most;
   if (!slice_lanes(C, cpg, full, &least, &most)) return false;
   const int tensors = bwd ? 2 : 1, kPer = bwd ? 4 : 8;
   const int wide = most < 8 ? most : 8 > least ? 8 : least;
-  auto fill = [&](int lanes, int TS, int threads, int CS) {
+  const int places = kHeldBytes / (kNT * 16 * tensors);  // per thread and tensor
+  auto fill = [&](int lanes, int TS, int CS) {
     pl->V = full;
     pl->TS = TS;
-    pl->threads = threads;
     pl->CS = CS;
     pl->slices = C / (lanes * full);
     pl->rpc = (P + CS - 1) / CS;
-    const long room = threads == 256 ? kHeldBytes : 2 * kHeldBytes, most_held = room / (threads * 16l * tensors);
     const long all = ((long)pl->rpc * lanes + TS - 1) / TS;
-    pl->hold = (int)(all < most_held ? all : most_held);
-    const long one = (long)pl->hold * threads * 16 * tensors;
-    pl->buffers = (int)(room / one < 4 ? room / one : 4);
-    const long teams = threads / TS, slots = (long)(threads == 256 ? 296 : 148) / CS * teams;  // teams at a time
-    long per = slots / pl->slices;
+    pl->more = all > places;
+    pl->hold = pl->more ? places - held_ring(bwd) : (int)all;
+    pl->buffers = pl->more ? 1 : places / pl->hold < 4 ? places / pl->hold : 4;
+    const long used = (pl->more ? places : pl->buffers * pl->hold) * (long)kNT * 16 * tensors;
+    const long teams = kNT / TS;
+    long per = 296 / CS * teams / pl->slices;  // teams at a time for each slice
     if (per > N) per = N;
     if (per < 1) per = 1;
     while (per * pl->slices % teams) ++per;
     pl->stride = (int)per;
     pl->blocks = (int)(per * pl->slices / teams * CS);
     pl->rows = (int)per * CS;
-    const long fold = bwd ? 2l * full * threads * 4 : 0;
-    pl->smem = (size_t)(pl->buffers * one > fold ? pl->buffers * one : fold);
+    const long fold = bwd ? 2l * full * kNT * 4 : 0;
+    pl->smem = (size_t)(used > fold ? used : fold);
   };
-  for (int TS = 32; TS <= 256; TS *= 2) {
+  for (int TS = 32; TS <= kNT; TS *= 2) {
     int lanes = most;
-    while (lanes > wide && ((long)P * lanes > (long)TS * kPer || (long)N * (C / (lanes * full)) * TS < 296 * 256)) lanes /= 2;
+    while (lanes > wide && ((long)P * lanes > (long)TS * kPer || (long)N * (C / (lanes * full)) * TS < 296 * kNT)) lanes /= 2;
     if ((long)P * lanes > (long)TS * kPer || lanes * full / cpg > 32) continue;
-    if (TS < 256 && (long)N * (C / (lanes * full)) * TS < 148 * 256) continue;  // few images: wider teams
-    fill(lanes, TS, 256, 1);
+    if (TS < kNT && (long)N * (C / (lanes * full)) * TS < 148 * kNT) continue;  // few images: wider teams
+    fill(lanes, TS, 1);
     return true;
   }
   if (wide * full / cpg > 32) return false;
-  for (int form = 0; form < 3; ++form) {
-    const int threads = form < 2 ? 256 : 512, top = form == 0 ? 8 : kMaxCluster;
-    const long room = threads == 256 ? kHeldBytes : 2 * kHeldBytes, items = (long)N * (C / (wide * full));
-    auto bytes = [&](int cs) { return (((long)(P + cs - 1) / cs * wide + threads - 1) / threads) * threads * 16 * tensors; };
-    int CS = 1;
-    while (CS < top && CS < P && (bytes(CS) > room || (items * CS < 148 && bytes(CS) > 16384))) CS *= 2;
-    if (bytes(CS) > room && form < 2) continue;
-    fill(wide, threads, threads, CS);
-    return true;
-  }
-  return false;
+  const long items = (long)N * (C / (wide * full)), slice = (long)P * wide * 16 * tensors;
+  int CS = 1;
+  while (CS < kMaxCluster && CS < P && slice / CS > 8192 && (items * CS < 128 || (items * CS < 256 && slice / CS > 4 * kHeldBytes))) CS *= 2;
+  fill(wide, kNT, CS);
+  return true;
 }
 
 GnPlan plan_gn(int dtype, int N, int P, int C, int groups, bool bwd) {
@@ -949,9 +1002,9 @@ GnPlan plan_gn(int dtype, int N, int P, int C, int groups, bool bwd) {
   }
   const size_t slab = image / pl.slices;
   const long items = (long)N * pl.slices;
+  // as few blocks to a cluster as give the SMs work: they wait for one another at every image
   pl.CS = 1;
-  while (pl.CS < kMaxCluster && pl.CS < P && (slab / pl.CS > 65536 || (items * pl.CS < 296 && slab / pl.CS > 8192))) pl.CS *= 2;
-  if (pl.CS > P) pl.CS = 1;
+  while (pl.CS < kMaxCluster && pl.CS < P && slab / pl.CS > 8192 && (items * pl.CS < 256 || (pl.CS < 4 && slab / pl.CS > 262144))) pl.CS *= 2;
   long most = kMaxBlocks / (pl.CS * pl.slices);
   if (most < 1) most = 1;
   if (most > N) most = N;
@@ -987,7 +1040,7 @@ int resident_clusters(K kernel, int CS, int threads, size_t smem, int* out) {
 template <typename T, int V, int ACT, bool BWD>
 int launch_gn(GnArgs& a, GnPlan& pl) {
   static bool ready[64];
-  static int resident[64][2][2][5];  // [device][FINE][512 threads][log2 CS]; 0: not asked yet
+  static int resident[64][2][2][5];  // [device][FINE][MORE][log2 CS]; 0: not asked yet
   int dev = 0;
   NF_CUDA(cudaGetDevice(&dev));
   if (dev < 0 || dev >= 64) return NF_EUNSUPPORTED;
@@ -1000,10 +1053,10 @@ int launch_gn(GnArgs& a, GnPlan& pl) {
   if (!ready[dev]) {
     int rc = allow(k, 200 * 1024);
     if constexpr (V * sizeof(T) == 16) {
-      if (rc == NF_OK) rc = allow(group_norm_held_kernel<T, V, ACT, BWD, true, 256, false>, kHeldBytes);
-      if (rc == NF_OK) rc = allow(group_norm_held_kernel<T, V, ACT, BWD, false, 256, false>, kHeldBytes);
-      if (rc == NF_OK) rc = allow(group_norm_held_kernel<T, V, ACT, BWD, true, 512, true>, 2 * kHeldBytes);
-      if (rc == NF_OK) rc = allow(group_norm_held_kernel<T, V, ACT, BWD, false, 512, true>, 2 * kHeldBytes);
+      if (rc == NF_OK) rc = allow(group_norm_held_kernel<T, V, ACT, BWD, true, false>, kHeldBytes);
+      if (rc == NF_OK) rc = allow(group_norm_held_kernel<T, V, ACT, BWD, false, false>, kHeldBytes);
+      if (rc == NF_OK) rc = allow(group_norm_held_kernel<T, V, ACT, BWD, true, true>, kHeldBytes);
+      if (rc == NF_OK) rc = allow(group_norm_held_kernel<T, V, ACT, BWD, false, true>, kHeldBytes);
     }
     if (rc != NF_OK) return rc;
     ready[dev] = true;
@@ -1011,14 +1064,14 @@ int launch_gn(GnArgs& a, GnPlan& pl) {
   if constexpr (V * sizeof(T) == 16) {
     if (pl.TS) {
       const bool fine = a.cpg < V;
-      auto held = fine ? (pl.threads == 512 ? group_norm_held_kernel<T, V, ACT, BWD, true, 512, true> : group_norm_held_kernel<T, V, ACT, BWD, true, 256, false>)
-                       : (pl.threads == 512 ? group_norm_held_kernel<T, V, ACT, BWD, false, 512, true> : group_norm_held_kernel<T, V, ACT, BWD, false, 256, false>);
+      auto held = fine ? (pl.more ? group_norm_held_kernel<T, V, ACT, BWD, true, true> : group_norm_held_kernel<T, V, ACT, BWD, true, false>)
+                       : (pl.more ? group_norm_held_kernel<T, V, ACT, BWD, false, true> : group_norm_held_kernel<T, V, ACT, BWD, false, false>);
       if (pl.CS > 1) {
         int lg = 0;
         while (1 << lg < pl.CS) ++lg;
-        int& most = resident[dev][fine][pl.threads == 512][lg];
+        int& most = resident[dev][fine][pl.more][lg];
         if (!most) {
-          const int rc = resident_clusters(held, pl.CS, pl.threads, pl.threads == 512 ? 2 * kHeldBytes : kHeldBytes, &most);
+          const int rc = resident_clusters(held, pl.CS, kNT, kHeldBytes, &most);
           if (rc != NF_OK) return rc;
         }
         if (most < 1) return NF_EUNSUPPORTED;
@@ -1028,7 +1081,7 @@ int launch_gn(GnArgs& a, GnPlan& pl) {
           pl.rows = a.stride * pl.CS;
         }
       }
-      nf_launch_cluster(held, (unsigned)pl.blocks, pl.threads, pl.smem, pl.CS, a);
+      nf_launch_cluster(held, (unsigned)pl.blocks, kNT, pl.smem, pl.CS, a);
       NF_LAUNCHED();
       return NF_OK;
     }

@@ -17,7 +17,8 @@ pytestmark = pytest.mark.gpu
 SHAPES = [  # N, P, C, groups
     (1, 1, 1, 1), (3, 1, 8, 4), (2, 1, 30, 1), (1, 5, 7, 7), (2, 9, 15, 5), (4, 16, 512, 32), (5, 4, 24, 3), (2, 49, 64, 32), (3, 100, 36, 9),
     (2, 63, 8, 8), (1, 784, 16, 2), (1, 1024, 64, 16), (300, 4, 64, 8), (1300, 1, 16, 4), (1, 333, 520, 13), (2, 7, 2056, 1), (1, 30, 4096, 1),
-    (1, 6, 8192, 4), (1, 5, 4099, 4099), (2, 3000, 32, 32), (1, 20000, 16, 4),
+    (1, 6, 8192, 4), (1, 5, 4099, 4099), (2, 3000, 32, 32), (1, 20000, 16, 4), (3, 50000, 64, 16),
+    (2, 41000, 64, 32), (5, 169, 20, 4), (3, 50, 6, 3), (2, 90, 30, 10),
 ]
 
 
