@@ -112,15 +112,17 @@ __global__ void __launch_bounds__(256) gemm_join_kernel(const float* __restrict_
 // piece of x serves kThinRows rows of weights.  Pairs of neighbouring products are added in one packed multiply-add; threads' sums meet by shuffles
 // and shared memory.
 constexpr int kThinRows = 4;
-// Up to four rows of bf16, eight of fp32: beyond, the tensor cores take the product sooner (8 x 8192 x 4096 bf16 38 us here, 18 there)
-template <typename T> constexpr int kThinMost = sizeof(T) == 4 ? 8 : 4;
+// Up to four rows of bf16, 24 of fp32: beyond, the tensor cores take the product sooner (8 x 8192 x 4096 bf16 38 us here, 18 there; 32 x 2344 x 7416
+// fp32 64 us there, 24 rows 49 us here)
+template <typename T> constexpr int kThinMost = sizeof(T) == 4 ? 24 : 4;
+template <typename T> constexpr int kThinRowsOfX = sizeof(T) == 4 ? 8 : 4;  // of one block; more rows take the weights through L2 again
 
 template <typename T, int MR>
 __global__ void __launch_bounds__(128) thin_kernel(const T* __restrict__ x, const T* __restrict__ w, int M, int N, int K, const Epilogue e) {
   nf_pdl_begin();
   constexpr int V = 16 / sizeof(T), NP = V / 2;
   __shared__ float sm[4][kThinRows * MR];
-  const int n0 = blockIdx.x * kThinRows;
+  const int n0 = blockIdx.x * kThinRows, m0 = blockIdx.y * MR;
   f32x2 acc[kThinRows][MR];
 #pragma unroll
   for (int j = 0; j < kThinRows; ++j)
@@ -146,7 +148,7 @@ __global__ void __launch_bounds__(128) thin_kernel(const T* __restrict__ x, cons
 #pragma unroll
     for (int m = 0; m < MR; ++m) {
       f32x2 a[NP];
-      pairs(x + (size_t)min(m, M - 1) * K + k, a, false);
+      pairs(x + (size_t)min(m0 + m, M - 1) * K + k, a, false);
 #pragma unroll
       for (int j = 0; j < kThinRows; ++j)
 #pragma unroll
@@ -166,15 +168,158 @@ __global__ void __launch_bounds__(128) thin_kernel(const T* __restrict__ x, cons
     }
   __syncthreads();
   if (threadIdx.x < kThinRows * MR) {
-    const int m = threadIdx.x / kThinRows, n = n0 + threadIdx.x % kThinRows;
+    const int m = m0 + threadIdx.x / kThinRows, n = n0 + threadIdx.x % kThinRows;
     if (m < M && n < N) finish<T>(e, (size_t)m * N + n, n, (sm[0][threadIdx.x] + sm[1][threadIdx.x]) + (sm[2][threadIdx.x] + sm[3][threadIdx.x]));
   }
 }
 
 template <typename T>
 int thin_product(const T* x, const T* w, int M, int N, int K, const Epilogue& e) {
-  auto k = M == 1 ? thin_kernel<T, 1> : M == 2 ? thin_kernel<T, 2> : M <= 4 ? thin_kernel<T, 4> : thin_kernel<T, kThinMost<T>>;
-  nf_launch(k, (unsigned)((N + kThinRows - 1) / kThinRows), 128, 0, x, w, M, N, K, e);
+  constexpr int most = kThinRowsOfX<T>;
+  auto k = M == 1 ? thin_kernel<T, 1> : M == 2 ? thin_kernel<T, 2> : M <= 4 ? thin_kernel<T, 4> : thin_kernel<T, most>;
+  nf_launch(k, dim3((N + kThinRows - 1) / kThinRows, (M + most - 1) / most), 128, 0, x, w, M, N, K, e);
+  NF_LAUNCHED();
+  return NF_OK;
+}
+
+// A few rows of A (MR to a block) through a matrix whose rows lie along q: the input gradients of small batches.  Again the matrix is all the traffic:
+// a lane keeps 16 bytes of columns, the eight warps of a block take rows r in turn, and A's values reach all lanes at once from shared memory.
+// Blocks share a column's rows (gridDim.z ranges, whose sums go to part[z][P][Q]) until the SMs have enough loads on their way.
+// 7 x 7416 x 2344 fp32 17 us, one row 10 us (the simple kernel 128 and 97, reading the matrix from memory 11); bf16 one or two rows 10 us, from three on
+// 16 here and 13 on the tensor cores.  fp32 24 rows 39 us, 32 on the tensor cores 62.
+constexpr int kAcrossRange = 256;  // rows of r whose part of A is in shared memory at a time
+template <typename T> constexpr int kAcrossMost = sizeof(T) == 4 ? 24 : 2;
+template <typename T> constexpr int kAcrossRows = sizeof(T) == 4 ? 8 : 2;
+
+template <typename T, int MR>
+__global__ void __launch_bounds__(256) across_kernel(const T* __restrict__ A, const T* __restrict__ B, int P, int Q, int R, float* part, const Epilogue e) {
+  nf_pdl_begin();
+  constexpr int V = 16 / sizeof(T), NP = V / 2, kCols = 32 * V;
+  __shared__ __align__(16) float sm[8 * MR * kCols > kAcrossRange * MR ? 8 * MR * kCols : kAcrossRange * MR];
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, p0 = blockIdx.y * MR, q = blockIdx.x * kCols + lane * V;
+  const int lo = (int)((long long)R * blockIdx.z / gridDim.z), hi = (int)((long long)R * (blockIdx.z + 1) / gridDim.z);
+  f32x2 acc[MR][NP];
+#pragma unroll
+  for (int m = 0; m < MR; ++m)
+#pragma unroll
+    for (int i = 0; i < NP; ++i) acc[m][i] = 0;
+  for (int c = lo; c < hi; c += kAcrossRange) {
+    const int n = min(kAcrossRange, hi - c);
+    __syncthreads();
+    if ((int)threadIdx.x < n) {
+      float a[MR];
+#pragma unroll
+      for (int m = 0; m < MR; ++m) a[m] = p0 + m < P ? ldf(A, (size_t)(p0 + m) * R + c + threadIdx.x) : 0.f;
+#pragma unroll
+      for (int m = 0; m < MR; ++m) sm[threadIdx.x * MR + m] = a[m];
+    }
+    __syncthreads();
+    if (q < Q) {  // whole: Q is a multiple of V
+#pragma unroll 8
+      for (int r = warp; r < n; r += 8) {
+        const T* at = B + (size_t)(c + r) * Q + q;
+        f32x2 b[NP];
+        if constexpr (sizeof(T) == 2) {
+          const uint4 u = __ldcs(reinterpret_cast<const uint4*>(at));
+          const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) b[i] = nf_pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+        } else {
+          const float4 u = __ldg(reinterpret_cast<const float4*>(at));
+          b[0] = nf_pack2(u.x, u.y);
+          b[1] = nf_pack2(u.z, u.w);
+        }
+#pragma unroll
+        for (int m = 0; m < MR; ++m) {
+          const float a = sm[r * MR + m];
+#pragma unroll
+          for (int i = 0; i < NP; ++i) acc[m][i] = nf_fma2(nf_pack2(a, a), b[i], acc[m][i]);
+        }
+      }
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int m = 0; m < MR; ++m)
+#pragma unroll
+    for (int i = 0; i < NP; i += 2) {
+      float4 v;
+      nf_unpack2(acc[m][i], v.x, v.y);
+      nf_unpack2(acc[m][i + 1], v.z, v.w);
+      *reinterpret_cast<float4*>(&sm[(warp * MR + m) * kCols + lane * V + 2 * i]) = v;
+    }
+  __syncthreads();
+  for (int i = threadIdx.x; i < MR * kCols; i += 256) {
+    const int p = p0 + i / kCols, col = blockIdx.x * kCols + i % kCols;
+    if (p >= P || col >= Q) continue;
+    float v = sm[i];
+#pragma unroll
+    for (int w = 1; w < 8; ++w) v += sm[w * MR * kCols + i];
+    const size_t at = (size_t)p * Q + col;
+    if (gridDim.z > 1) part[(size_t)blockIdx.z * P * Q + at] = v;
+    else finish<T>(e, at, col, v);
+  }
+}
+
+template <typename T>
+bool across(int P, int Q) { return P <= kAcrossMost<T> && Q % (16 / (int)sizeof(T)) == 0; }
+// Ranges of r: four blocks for each SM, 64 rows each at least and 4096 (512 steps of a running sum) at most
+template <typename T>
+int across_splits(int P, int Q, int R) {
+  const int blocks = (Q + 512 / (int)sizeof(T) - 1) / (512 / (int)sizeof(T)) * ((P + kAcrossRows<T> - 1) / kAcrossRows<T>);
+  int s = 592 / blocks;
+  if (s > R / 64) s = R / 64;
+  if (s < (R - 1) / 4096 + 1) s = (R - 1) / 4096 + 1;
+  return s < 65535 ? s : 65535;
+}
+
+// Sums of few terms (R of them, RR at most): the weight gradients of small batches, where writing the result is all the traffic.  A thread keeps its four
+// columns of B in registers for 16 rows of the result; A's 64 columns lie in shared memory.  7416 x 2344 of 7 rows 14 us fp32, 13 bf16 (48 and 21 before,
+// writing 10.8); of 16 rows fp32 24 us (49 by the simple kernel), bf16 25 us (21 on the tensor cores, which take over from nine).
+constexpr int kOuterRows = 64;
+template <typename T> constexpr int kOuterMost = sizeof(T) == 4 ? 16 : 8;
+
+template <typename T, int RR>
+__global__ void __launch_bounds__(256) outer_kernel(const T* __restrict__ A, const T* __restrict__ B, int P, int Q, int R, const Epilogue e) {
+  nf_pdl_begin();
+  __shared__ float as[kOuterRows][RR];
+  const int p0 = blockIdx.x * kOuterRows, q = blockIdx.y * 256 + threadIdx.x % 64 * 4;
+  for (int i = threadIdx.x; i < kOuterRows * RR; i += 256) {
+    const int r = i / kOuterRows, p = i % kOuterRows;
+    as[p][r] = r < R && p0 + p < P ? ldf(A, (size_t)r * P + p0 + p) : 0.f;
+  }
+  f32x2 b[RR][2];
+#pragma unroll
+  for (int r = 0; r < RR; ++r) {
+    float v[4] = {};
+    if (r < R && q < Q)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = ldf(B, (size_t)r * Q + q + j);
+    b[r][0] = nf_pack2(v[0], v[1]);
+    b[r][1] = nf_pack2(v[2], v[3]);
+  }
+  __syncthreads();
+  if (q >= Q) return;  // whole: Q is a multiple of four
+#pragma unroll 4
+  for (int p = threadIdx.x / 64; p < min(kOuterRows, P - p0); p += 4) {
+    f32x2 lo = 0, hi = 0;
+#pragma unroll
+    for (int r = 0; r < RR; ++r) {
+      const float a = as[p][r];
+      lo = nf_fma2(nf_pack2(a, a), b[r][0], lo);
+      hi = nf_fma2(nf_pack2(a, a), b[r][1], hi);
+    }
+    float4 v;
+    nf_unpack2(lo, v.x, v.y);
+    nf_unpack2(hi, v.z, v.w);
+    *reinterpret_cast<float4*>(reinterpret_cast<float*>(e.out) + (size_t)(p0 + p) * Q + q) = v;
+  }
+}
+
+template <typename T>
+int outer_product(const T* A, const T* B, int P, int Q, int R, const Epilogue& e) {
+  auto k = R <= 4 ? outer_kernel<T, 4> : R <= 8 ? outer_kernel<T, 8> : outer_kernel<T, kOuterMost<T>>;
+  nf_launch(k, dim3((P + kOuterRows - 1) / kOuterRows, (Q + 255) / 256), 256, 0, A, B, P, Q, R, e);
   NF_LAUNCHED();
   return NF_OK;
 }
@@ -419,11 +564,14 @@ struct Product {
   int b_len() const { return b_along_r ? R : Q; }
 };
 
-// bf16: always (a 128 x 64 x 10 product took 6 us there and 10 us on the CUDA cores).  fp32: from 2^26 multiply-adds on, where what
-// cutting the operands into parts costs is earned back (256 x 256 x 256 16 us there, 9 us here; 512 x 512 x 512 17 us and 24 us).
-// Thin products stay off: their traffic, three parts written and read, costs more than the sums.
+// bf16: always (a 128 x 64 x 10 product took 6 us there and 10 us on the CUDA cores).  fp32: from 2^26 multiply-adds on, counted in the 64 x 64 tiles of
+// the simple kernel, where what cutting the operands into parts costs is earned back (256 x 256 x 256 16 us there, 9 us here; 512 x 512 x 512 17 us and
+// 24 us) -- with a side of a few too: 100000 x 512 x 10 195 us there, 301 here, its gradients 65 and 155 us there, 149 and 350 here.
 bool on_tensor_cores(int dtype, const Product& d) {
-  return dtype == NF_BF16 || ((double)d.P * d.Q * d.R >= 67108864.0 && d.P >= 64 && d.Q >= 64 && d.R >= 64);
+  return dtype == NF_BF16 || (double)nf_align_up(d.P, 64) * (double)nf_align_up(d.Q, 64) * d.R >= 67108864.0;
+}
+bool few_across(int dtype, const Product& d) {
+  return d.a_along_r && !d.b_along_r && (dtype == NF_F32 ? across<float>(d.P, d.Q) : across<bf16>(d.P, d.Q));
 }
 bool needs_copy(int dtype, int len) { return dtype == NF_F32 || len % 8; }
 size_t copy_bytes(int dtype, int rows, int len) {
@@ -441,6 +589,10 @@ size_t product_bytes(int dtype, const Product& d) {
   const bool tc = on_tensor_cores(dtype, d);
   const int s = tc ? nf_gemm_splits(d.P, d.Q, d.R, dtype == NF_F32 ? 3 : 1) : simple_splits(d.P, d.Q, d.R);
   size_t b = s > 1 ? (size_t)s * d.P * d.Q * 4 : 0;
+  if (few_across(dtype, d)) {
+    const int n = dtype == NF_F32 ? across_splits<float>(d.P, d.Q, d.R) : across_splits<bf16>(d.P, d.Q, d.R);
+    return (size_t)n * d.P * d.Q * 4;
+  }
   if (tc) b += copy_bytes(dtype, d.a_rows(), d.a_len()) + copy_bytes(dtype, d.b_rows(), d.b_len());
   return b;
 }
@@ -466,6 +618,17 @@ int simple_product(const Product& d, const float* A, const float* B, float* part
 }
 
 template <typename T>
+int across_product(const T* A, const T* B, float* part, const Product& d, const Epilogue& e) {
+  const int splits = across_splits<T>(d.P, d.Q, d.R), cols = 512 / (int)sizeof(T);
+  auto k = d.P == 1 ? across_kernel<T, 1> : d.P == 2 ? across_kernel<T, 2> : across_kernel<T, kAcrossRows<T>>;
+  if constexpr (sizeof(T) == 4)
+    if (d.P == 3 || d.P == 4) k = across_kernel<T, 4>;
+  nf_launch(k, dim3((d.Q + cols - 1) / cols, (d.P + kAcrossRows<T> - 1) / kAcrossRows<T>, splits), 256, 0, A, B, d.P, d.Q, d.R, part, e);
+  NF_LAUNCHED();
+  return splits > 1 ? join<T>(part, splits, d.P, d.Q, e) : NF_OK;
+}
+
+template <typename T>
 int operand(const void* src, int rows, int len, bool along_r, char*& scratch, GemmOperand* o) {
   const int dtype = sizeof(T) == 4 ? NF_F32 : NF_BF16;
   *o = {(const bf16*)src, (size_t)len, 0, along_r};
@@ -487,6 +650,8 @@ int product(const Product& d, const void* A, const void* B, void* scratch, const
   if (d.a_along_r && d.R <= 64 && d.Q <= 64 && d.R * d.Q <= kRowsMost) return rows_product<T>((const T*)A, (const T*)B, d.P, d.Q, d.R, d.b_along_r, e);
   if (d.P <= kThinMost<T> && d.a_along_r && d.b_along_r && d.R % (16 / (int)sizeof(T)) == 0)
     return thin_product<T>((const T*)A, (const T*)B, d.P, d.Q, d.R, e);
+  if (few_across(dtype, d)) return across_product<T>((const T*)A, (const T*)B, (float*)scratch, d, e);
+  if (!d.a_along_r && !d.b_along_r && e.out_f32 && d.R <= kOuterMost<T> && d.Q % 4 == 0) return outer_product<T>((const T*)A, (const T*)B, d.P, d.Q, d.R, e);
   if constexpr (sizeof(T) == 4) {
     if (!on_tensor_cores(dtype, d)) return simple_product(d, (const float*)A, (const float*)B, (float*)scratch, e);
   }

@@ -21,6 +21,11 @@ SHAPES = [  # M, K, N
     (3600, 72, 1030), (1800, 2000, 2056), (1801, 2009, 2051), (20000, 128, 136),
 ]
 
+SHAPES += [  # few rows forwards and backwards (whole and odd widths, sums cut into ranges and not), few terms, a thin side of many rows
+    (1, 4, 1), (2, 264, 63), (3, 1000, 65), (4, 516, 700), (6, 4096, 4100), (9, 260, 5000), (15, 1001, 130), (23, 72, 2056), (24, 2048, 1000), (25, 128, 640),
+    (16, 1028, 68), (17, 1028, 68), (12, 63, 77), (20000, 512, 10), (20000, 10, 512), (30000, 3, 600), (5, 20000, 36), (4, 36, 20000),
+]
+
 
 @pytest.fixture(scope="module")
 def env():
