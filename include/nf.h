@@ -328,7 +328,7 @@ int nf_conv3x3_wgrad_static(int dtype, const void* x, const void* g, int N, int 
  * activation cache in 8 bits.  (The paper's networks are VGG and ResNet shapes: a classifier of linear layers with dropout stands
  * behind their last block, 1x1 convolutions are linear layers over pixels, and at the batch sizes of a few images that small memory
  * budgets force, group normalisation replaces batch statistics.)  All pointers device unless said otherwise, 16-byte aligned, tensors dense and
- * channels-last; outputs must not share memory with inputs except where a call says so.  Parameters, statistics and parameter gradients are float,
+ * channels-last; outputs must not share memory with inputs or scratch except where a call says so.  Parameters, statistics and parameter gradients are float,
  * activations and their gradients of `dtype`, linear weights of `dtype`.  Arithmetic and sums in fp32 or more, each output rounded once.
  * Results do not depend on launch order: the same call on the same data gives the same bits.  Asynchronous on the library's stream, and
  * recordable into a CUDA graph after a first eager call with the same arguments.  Concurrent calls need scratch of their own. */
@@ -337,8 +337,10 @@ enum nf_act { NF_ACT_NONE = 0, NF_ACT_RELU = 1, NF_ACT_SILU = 2, NF_ACT_GELU = 3
 /* Group normalisation with the activation behind it.  x, y: [N][P][C], P pixels per image; the C channels form `groups` groups of
  * neighbours; gamma, beta: [C]; mean, rstd: [N][groups] (written, for the backward pass):
  *   y = act(gamma xh + beta),  xh = (x - mean) rstd,  rstd = 1 / sqrt(variance + eps), biased variance over P * C/groups values.
- * Backward: dy the gradient at y; dx the gradient at x; dgamma, dbeta: [C].  Needs nf_group_norm_scratch_bytes() of scratch (overwritten).
- * NF_EINVAL: sizes < 1, C not a multiple of groups, eps not above 0; NF_EUNSUPPORTED: more than 4096 channels in a group. */
+ * Backward: dy the gradient at y; dx the gradient at x; dgamma, dbeta: [C].  Needs nf_group_norm_scratch_bytes() of scratch (overwritten).  A ReLU is
+ * open in it where gamma xh + beta is above 0 with every operation rounded to fp32 by itself.
+ * NF_EINVAL: sizes < 1, C not a multiple of groups, eps not above 0; NF_EUNSUPPORTED: more than 4096 channels in a group,
+ * 2^24 channels, 2^30 images or pixels. */
 int nf_group_norm_forward(int dtype, const void* x, const float* gamma, const float* beta, int N, int P, int C, int groups, float eps, int act,
                           void* y, float* mean, float* rstd);
 size_t nf_group_norm_scratch_bytes(int dtype, int N, int P, int C, int groups);
@@ -353,7 +355,8 @@ int nf_group_norm_backward(int dtype, const void* x, const void* dy, const float
  *   nf_linear_dgrad: dx = g w [M][K].
  *   nf_linear_wgrad: dw = g^T x, float [N][K]; db = column sums of g, float [N], or NULL.
  * All but nf_act_backward need nf_linear_scratch_bytes() of scratch (overwritten).  fp32 operands have to be finite and below 2^127 in
- * magnitude: an infinity among them may give NaN instead of an infinity. */
+ * magnitude: an infinity among them may give NaN instead of an infinity; operands below 2^-102 may lose digits.  NF_EINVAL: sizes < 1; NF_EUNSUPPORTED: sizes
+ * above 2^30, results of more than 2^22 - 64 columns (N forward, K of dx and dw). */
 int nf_linear_forward(int dtype, const void* x, const void* w, const float* bias, const void* residual, int M, int K, int N, int act, void* scratch,
                       size_t scratch_bytes, void* pre, void* y);
 int nf_act_backward(int dtype, int act, const void* saved, const void* dy, long long n, void* g);

@@ -117,7 +117,7 @@ __device__ __forceinline__ void tile_to_rows(uint32_t tile, T* dst, int row0, in
     }
 }
 
-// One branch per activation, not one per value: with the branch inside the loop the 1x1 product of 200704 x 256 x 256 took 136 us for XX
+// One branch per activation, not one per value: with the branch inside the loop the 1x1 product of 200704 x 256 x 256 took 136 us for 65
 template <typename T, int CH>
 __device__ __forceinline__ void activate(float (&v)[CH], int act) {
   if (act == NF_ACT_RELU) {

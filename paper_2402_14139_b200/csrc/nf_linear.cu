@@ -693,6 +693,7 @@ void column_sums(const SumPlan& s, const T* g, int M, int N, float* part) {
   nf_launch(s.V == 8 ? column_sums_kernel<T, 8> : column_sums_kernel<T, 1>, dim3(s.blocks, s.cols), s.threads, 0, g, M, N, s.lx, part);
 }
 
+bool large(int M, int K, int N) { return M > 1 << 30 || K > 1 << 30 || N > 1 << 30; }  // positions run on beyond the last one, in 32 bits
 bool sizes_ok(int dtype, int M, int K, int N) { return (dtype == NF_F32 || dtype == NF_BF16) && M >= 1 && K >= 1 && N >= 1; }
 
 Product forward_of(int M, int K, int N) { return {M, N, K, true, true}; }
@@ -702,7 +703,7 @@ Product wgrad_of(int M, int K, int N) { return {N, K, M, false, false}; }
 }  // namespace
 
 extern "C" size_t nf_linear_scratch_bytes(int dtype, int M, int K, int N) {
-  if (!sizes_ok(dtype, M, K, N)) return 0;
+  if (!sizes_ok(dtype, M, K, N) || large(M, K, N)) return 0;
   size_t b = 0;
   for (const Product& d : {forward_of(M, K, N), dgrad_of(M, K, N), wgrad_of(M, K, N)}) {
     const size_t n = product_bytes(dtype, d);
@@ -720,7 +721,12 @@ extern "C" int nf_linear_forward(int dtype, const void* x, const void* w, const 
     if (nf_overlap(o, yb, x, xb) || nf_overlap(o, yb, w, wb) || nf_overlap(o, yb, residual, yb) || nf_overlap(o, yb, bias, (size_t)N * 4))
       return NF_EINVAL;
   if (nf_overlap(y, yb, pre, yb)) return NF_EINVAL;
-  if (scratch_bytes < nf_linear_scratch_bytes(dtype, M, K, N)) return NF_ENOWS;
+  if (large(M, K, N)) return NF_EUNSUPPORTED;
+  const size_t need = nf_linear_scratch_bytes(dtype, M, K, N);
+  if (scratch_bytes < need) return NF_ENOWS;
+  for (const void* t : {(const void*)y, (const void*)pre, residual})
+    if (nf_overlap(scratch, need, t, yb)) return NF_EINVAL;
+  if (nf_overlap(scratch, need, x, xb) || nf_overlap(scratch, need, w, wb) || nf_overlap(scratch, need, bias, (size_t)N * 4)) return NF_EINVAL;
   const Epilogue e{bias, residual, act, pre, y, 0};
   const Product d = forward_of(M, K, N);
   return dtype == NF_F32 ? product<float>(d, x, w, scratch, e) : product<bf16>(d, x, w, scratch, e);
@@ -731,7 +737,10 @@ extern "C" int nf_linear_dgrad(int dtype, const void* g, const void* w, int M, i
   if (((uintptr_t)g | (uintptr_t)w | (uintptr_t)scratch | (uintptr_t)dx) & 15) return NF_EALIGN;
   const size_t es = nf_esize(dtype), xb = es * M * K;
   if (nf_overlap(dx, xb, g, es * M * N) || nf_overlap(dx, xb, w, es * N * K)) return NF_EINVAL;
-  if (scratch_bytes < nf_linear_scratch_bytes(dtype, M, K, N)) return NF_ENOWS;
+  if (large(M, K, N)) return NF_EUNSUPPORTED;
+  const size_t need = nf_linear_scratch_bytes(dtype, M, K, N);
+  if (scratch_bytes < need) return NF_ENOWS;
+  if (nf_overlap(scratch, need, dx, xb) || nf_overlap(scratch, need, g, es * M * N) || nf_overlap(scratch, need, w, es * N * K)) return NF_EINVAL;
   const Epilogue e{nullptr, nullptr, NF_ACT_NONE, nullptr, dx, 0};
   const Product d = dgrad_of(M, K, N);
   return dtype == NF_F32 ? product<float>(d, g, w, scratch, e) : product<bf16>(d, g, w, scratch, e);
@@ -745,7 +754,12 @@ extern "C" int nf_linear_wgrad(int dtype, const void* x, const void* g, int M, i
   if (nf_overlap(dw, wb, x, es * M * K) || nf_overlap(dw, wb, g, es * M * N) || nf_overlap(db, bb, x, es * M * K) ||
       nf_overlap(db, bb, g, es * M * N) || nf_overlap(dw, wb, db, bb))
     return NF_EINVAL;
-  if (scratch_bytes < nf_linear_scratch_bytes(dtype, M, K, N)) return NF_ENOWS;
+  if (large(M, K, N)) return NF_EUNSUPPORTED;
+  const size_t need = nf_linear_scratch_bytes(dtype, M, K, N);
+  if (scratch_bytes < need) return NF_ENOWS;
+  if (nf_overlap(scratch, need, dw, wb) || nf_overlap(scratch, need, db, bb) || nf_overlap(scratch, need, x, es * M * K) ||
+      nf_overlap(scratch, need, g, es * M * N))
+    return NF_EINVAL;
   const SumPlan sums = sum_plan(M, N);
   if (db && sums.cols > 65535) return NF_EUNSUPPORTED;
   const Epilogue e{nullptr, nullptr, NF_ACT_NONE, nullptr, dw, 1};

@@ -18,6 +18,8 @@
 
 #include <cuda.h>
 
+#include <initializer_list>
+
 #include "nf_act.cuh"
 #include "nf_ldst.cuh"
 #include "nf_ptx.cuh"
@@ -578,7 +580,7 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a)
 
   // Read one image ahead: its statistics (backward), or the pivot of this thread's group, the group's first channel at the block's first pixel
   float2 ahead = make_float2(0.f, 0.f);
-  const int pivot_at = (p0 < a.P ? p0 : a.P - 1) * a.C + c0 + tc / lo * a.cpg;
+  const size_t pivot_at = (size_t)(p0 < a.P ? p0 : a.P - 1) * a.C + c0 + tc / lo * a.cpg;
   auto look = [&](int n) {
     if (FINE || n >= a.N) return;
     if constexpr (BWD) {
@@ -698,7 +700,7 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a)
     const float M = (float)a.P * a.cpg;
     // Group totals (A, B) of a block's pixels -> mean, squared deviations; statistics -> what pass two wants
     auto about = [&](float& A, float& B, float k, int pixels) {
-      const float d = pixels ? A / ((float)pixels * a.cpg) : 0.f;  // counts are below 2^24: the pixels fit shared memory
+      const float d = pixels ? A / ((float)pixels * a.cpg) : 0.f;
       B = fmaf(-A, d, B);
       if (B < 0.f) B = 0.f;  // a NaN stays one
       A = k + d;
@@ -1016,6 +1018,9 @@ GnPlan plan_gn(int dtype, int N, int P, int C, int groups, bool bwd) {
   return pl;
 }
 
+// Counts of images and pixels run on in steps beyond the last one, channels are doubled: all in 32 bits
+bool gn_size_ok(int N, int P, int C, int groups) { return C / groups <= kMaxCs && N <= 1 << 30 && P <= 1 << 30 && C <= 1 << 24; }
+
 bool gn_args_ok(int dtype, int N, int P, int C, int groups) {
   return (dtype == NF_F32 || dtype == NF_BF16) && N >= 1 && P >= 1 && C >= 1 && groups >= 1 && C % groups == 0;
 }
@@ -1125,7 +1130,7 @@ extern "C" int nf_group_norm_forward(int dtype, const void* x, const float* gamm
                                      float eps, int act, void* y, float* mean, float* rstd) {
   if (!x || !gamma || !beta || !y || !mean || !rstd || !gn_args_ok(dtype, N, P, C, groups) || !nf_act_ok(act) || !(eps > 0.f)) return NF_EINVAL;
   if (((uintptr_t)x | (uintptr_t)gamma | (uintptr_t)beta | (uintptr_t)y | (uintptr_t)mean | (uintptr_t)rstd) & 15) return NF_EALIGN;
-  if (C / groups > kMaxCs) return NF_EUNSUPPORTED;
+  if (!gn_size_ok(N, P, C, groups)) return NF_EUNSUPPORTED;
   const size_t bytes = (size_t)N * P * C * nf_esize(dtype);
   if (nf_overlap(x, bytes, y, bytes)) return NF_EINVAL;
   GnPlan pl = plan_gn(dtype, N, P, C, groups, false);
@@ -1136,7 +1141,7 @@ extern "C" int nf_group_norm_forward(int dtype, const void* x, const float* gamm
 }
 
 extern "C" size_t nf_group_norm_scratch_bytes(int dtype, int N, int P, int C, int groups) {
-  if (!gn_args_ok(dtype, N, P, C, groups) || C / groups > kMaxCs) return 0;
+  if (!gn_args_ok(dtype, N, P, C, groups) || !gn_size_ok(N, P, C, groups)) return 0;
   return (size_t)plan_gn(dtype, N, P, C, groups, true).rows * 2 * C * sizeof(float);
 }
 
@@ -1149,11 +1154,16 @@ extern "C" int nf_group_norm_backward(int dtype, const void* x, const void* dy, 
   if (((uintptr_t)x | (uintptr_t)dy | (uintptr_t)gamma | (uintptr_t)beta | (uintptr_t)mean | (uintptr_t)rstd | (uintptr_t)scratch |
        (uintptr_t)dx | (uintptr_t)dgamma | (uintptr_t)dbeta) & 15)
     return NF_EALIGN;
-  if (C / groups > kMaxCs) return NF_EUNSUPPORTED;
+  if (!gn_size_ok(N, P, C, groups)) return NF_EUNSUPPORTED;
   const size_t bytes = (size_t)N * P * C * nf_esize(dtype);
   GnPlan pl = plan_gn(dtype, N, P, C, groups, true);
   if (scratch_bytes < (size_t)pl.rows * 2 * C * sizeof(float)) return NF_ENOWS;
+  const size_t used = (size_t)pl.rows * 2 * C * sizeof(float);
   if (nf_overlap(x, bytes, dx, bytes) || nf_overlap(dy, bytes, dx, bytes)) return NF_EINVAL;
+  for (const void* t : {x, dy, (const void*)dx})
+    if (nf_overlap(scratch, used, t, bytes)) return NF_EINVAL;
+  for (const void* t : {(const void*)dgamma, (const void*)dbeta, (const void*)gamma, (const void*)beta})
+    if (nf_overlap(scratch, used, t, (size_t)C * 4)) return NF_EINVAL;
   GnArgs a{};
   if (fill_gn(a, pl, N, P, C, groups, act) != NF_OK) return NF_ECUDA;
   a.x = x; a.dy = dy; a.gamma = gamma; a.beta = beta; a.out = dx; a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);

@@ -179,3 +179,44 @@ def test_offsets_beyond_32_bits(env):
     y, mean, rstd = torch.empty_like(x), torch.empty((N, G), device="cuda"), torch.empty((N, G), device="cuda")
     nf.nf_group_norm_forward(1, x, ga, be, G, 1e-5, "none", y, mean, rstd)
     assert torch.equal(y[0], y[-1]) and torch.equal(mean[0], mean[-1]) and float(y[0].float().std()) > 0.99 and float(y[1].abs().max()) == 0
+
+
+def test_an_image_of_more_than_2_to_31_elements(env):
+    """Offsets beyond 32 bits, in the held form's last block as well.  A thread adds P / 16 pixels' pieces of 8 over 256 threads of 8 to a pixel: its
+    chain is n = P / 512 steps per channel pair and T = n + 40 roundings with the joins, each of them independent and at most u of a running sum: a sum is
+    off by less than e = 8 sqrt(T) u of what its terms' magnitudes come to.  Distances from a pivot below 6 sigma have a mean magnitude below 7 and a mean
+    square below 37: a mean is off by 7 e, a second moment by 37 e."""
+    nf, torch = env
+    P, C, G = 37_000_001, 64, 16
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x = torch.empty((1, P, C), dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    dy = torch.empty((1, P, C), dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    ga, be = torch.linspace(0.5, 1.5, C, device="cuda"), torch.linspace(-1, 1, C, device="cuda")
+    y, dx = torch.full_like(x, float("nan")), torch.full_like(x, float("nan"))
+    mean, rstd = (torch.full((1, G), float("nan"), device="cuda") for _ in range(2))
+    nf.nf_group_norm_forward(1, x, ga, be, G, 1e-5, "none", y, mean, rstd)
+    scratch = torch.empty(nf.nf_group_norm_scratch_bytes(1, 1, P, C, G), dtype=torch.uint8, device="cuda")
+    dga, dbe = torch.empty(C, device="cuda"), torch.empty(C, device="cuda")
+    nf.nf_group_norm_backward(1, x, dy, ga, be, mean, rstd, "none", scratch, dx, dga, dbe)
+    s = [torch.zeros(C, dtype=torch.float64, device="cuda") for _ in range(4)]          # sums of x, x^2, dy, dy x
+    for p in range(0, P, 1 << 20):
+        v, d = x[0, p:p + (1 << 20)].double(), dy[0, p:p + (1 << 20)].double()
+        for t, w in zip(s, (v, v * v, d, d * v)):
+            t += w.sum(0)
+        assert bool(y[0, p:p + (1 << 20)].isfinite().all()) and bool(dx[0, p:p + (1 << 20)].isfinite().all())
+    M, grp, e = P * (C // G), lambda t: t.reshape(G, C // G).sum(1), 8 * np.sqrt(P / 512 + 40) * U
+    wm = grp(s[0]) / M
+    wr = 1 / (grp(s[1]) / M - wm * wm + 1e-5).sqrt()
+    assert float((mean[0] - wm).abs().max()) <= 7 * e and float((rstd[0] - wr).abs().max()) <= 0.51 * (37 + 2 * 49) * e
+    m, r = (t.repeat_interleave(C // G) for t in (wm, wr))
+    gd, bd = ga.double(), be.double()
+    wdb, wdg = s[2], (s[3] - m * s[2]) * r
+    m1, m2 = (grp(gd * t).repeat_interleave(C // G) / M for t in (wdb, wdg))
+    off = 0.51 * (37 + 2 * 49) * e                                                       # of xh, for each of 1 + |xh|
+    for p in (0, P // 2, 34_700_000, P - 2000):
+        xh = (x[0, p:p + 2000].double() - m) * r
+        d = dy[0, p:p + 2000].double()
+        wy, wdx = xh * gd + bd, r * (gd * d - m1 - xh * m2)
+        assert bool(((y[0, p:p + 2000] - wy).abs() <= wy.abs() * 2.0 ** -8 + 1.5 * off * (1 + xh.abs())).all())
+        assert bool(((dx[0, p:p + 2000] - wdx).abs() <= wdx.abs() * 2.0 ** -8 + 3 * off * (1 + xh.abs() + d.abs())).all())
+    assert nf.nf_op_status() == 0

@@ -62,6 +62,31 @@ def test_refusals(nf):
     assert n > 100
 
 
+def test_refusals_of_sizes_and_of_scratch_in_use(nf):
+    """Sizes whose counters would pass 32 bits, and scratch that lies in a tensor of the call."""
+    L, E, U = nf.lib(), nf.NF_EINVAL, nf.NF_EUNSUPPORTED
+    big = (1 << 30) + 1
+    far = [C.c_void_p(a.value << 24) for a in A]       # 2^44 apart: the sizes below do not make them overlap
+    for n, p, c, g in ((big, 1, 1, 1), (1, big, 1, 1), (0x7fffffff, 1, 1, 1), (1, 0x7fffffff, 1, 1), (1, 1, 1 << 25, 1 << 25)):
+        assert L.nf_group_norm_forward(1, far[0], far[1], far[2], n, p, c, g, 1e-5, 1, far[3], far[4], far[5]) == U
+        assert L.nf_group_norm_backward(1, far[0], far[1], far[2], far[3], far[4], far[5], n, p, c, g, 1, far[6], 1 << 40, far[7], far[8], far[9]) == U
+        assert L.nf_group_norm_scratch_bytes(1, n, p, c, g) == 0
+    for m, k, n in ((big, 1, 1), (1, big, 1), (1, 1, big)):
+        assert L.nf_linear_forward(1, far[0], far[1], None, None, m, k, n, 0, far[2], 1 << 40, None, far[3]) == U
+        assert L.nf_linear_dgrad(1, far[0], far[1], m, k, n, far[2], 1 << 40, far[3]) == U
+        assert L.nf_linear_wgrad(1, far[0], far[1], m, k, n, far[2], 1 << 40, far[3], None) == U
+        assert L.nf_linear_scratch_bytes(1, m, k, n) == 0
+    gsb, lsb = L.nf_group_norm_scratch_bytes(1, 2, 4, 16, 4), L.nf_linear_scratch_bytes(1, 4, 16, 8)
+    for k in (0, 1, 2, 3, 7, 8, 9):
+        assert L.nf_group_norm_backward(1, *A[:6], 2, 4, 16, 4, 1, A[k], gsb, *A[7:10]) == E, k
+    for k in (0, 1, 2, 3, 5, 6):
+        assert L.nf_linear_forward(1, *A[:4], 4, 16, 8, 1, A[k], lsb, A[5], A[6]) == E, k
+    for k in (0, 1, 3):
+        assert L.nf_linear_dgrad(1, A[0], A[1], 4, 16, 8, A[k], lsb, A[3]) == E, k
+    for k in (0, 1, 3, 4):
+        assert L.nf_linear_wgrad(1, A[0], A[1], 4, 16, 8, A[k], lsb, A[3], A[4]) == E, k
+
+
 def test_scratch_sizes_are_host_only(nf):
     L = nf.lib()
     assert L.nf_linear_scratch_bytes(1, 0, 16, 8) == 0 and L.nf_linear_scratch_bytes(5, 4, 16, 8) == 0
