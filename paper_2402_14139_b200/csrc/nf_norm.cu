@@ -459,7 +459,7 @@ __device__ __forceinline__ void copies_wait(int behind) {  // all but the latest
 }
 
 // Places per thread and tensor that the rest of a large image passes through: 32 KB on their way in a block, two blocks on an SM.  64 images of
-// 224x224x64 forward: 4 places 222 us, 6 and more 208 to 212.
+// 224x224x64 forward: 4 places 7% slower, 6 and more the same.
 __host__ __device__ constexpr int held_ring(bool bwd) { return bwd ? 4 : 8; }
 
 template <typename T, int V, int ACT, bool BWD, bool FINE, bool MORE>
@@ -513,7 +513,8 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a)
     }
     copies_end();
   }
-  // The ring's loads run kRing pieces ahead of their use, through both passes and from one image to the next: (image, pass, pieces left, where)
+  // The ring's loads run kRing pieces ahead of their use, through both passes and from one image to the next: (image, pass, pieces left, where).  The
+  // second pass goes backwards, from what L2 has had last.
   const uint32_t ring0 = slot0 + kTensors * a.hold * kstep;
   const size_t ring_at = (size_t)tr * a.C + a.hold * row_step;
   int ring_n = first, ring_left = ks;
@@ -521,25 +522,28 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a)
   uint32_t ring_slot = 0;  // place of the next piece to be used
   const T* ring_x = x + (size_t)first * image + ring_at;
   const T* ring_dy = BWD ? dy + (size_t)first * image + ring_at : nullptr;
+  const ptrdiff_t forth = (ptrdiff_t)row_step;
+  const size_t ring_end = ks ? (ks - 1) * row_step : 0;  // its last piece, from its first
   auto ring_fill = [&](uint32_t place) {
     if (ring_n < a.N && ks) {
       copy16(ring0 + place * kstep, ring_x);
-      ring_x += row_step;
+      ring_x += ring_second ? -forth : forth;
       if constexpr (BWD) {
         copy16(ring0 + (kRing + place) * kstep, ring_dy);
-        ring_dy += row_step;
+        ring_dy += ring_second ? -forth : forth;
       }
       if (--ring_left == 0) {
         ring_left = ks;
         if (ring_second) ring_n += a.stride;
         ring_second = !ring_second;
-        ring_x = x + (size_t)ring_n * image + ring_at;
-        if constexpr (BWD) ring_dy = dy + (size_t)ring_n * image + ring_at;
+        const size_t at = (size_t)ring_n * image + ring_at + (ring_second ? ring_end : 0);
+        ring_x = x + at;
+        if constexpr (BWD) ring_dy = dy + at;
       }
     }
     copies_end();
   };
-  auto ring_use = [&](auto&& f) {  // f(x, dy) for each of this pass's pieces
+  auto ring_use = [&](auto&& f, ptrdiff_t way) {  // f(x, dy) for each of this pass's pieces, way from one to the next
     auto step = [&](auto&& fill) {
       asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
       Raw<T, V> v, g;
@@ -552,10 +556,10 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a)
     };
     auto along = [&] {  // within a pass the loads move on by rows
       copy16(ring0 + ring_slot * kstep, ring_x);
-      ring_x += row_step;
+      ring_x += way;
       if constexpr (BWD) {
         copy16(ring0 + (kRing + ring_slot) * kstep, ring_dy);
-        ring_dy += row_step;
+        ring_dy += way;
       }
       copies_end();
     };
@@ -654,7 +658,7 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a)
       }
       for (k += last_held; k > 0; --k, at += kstep) one(at);
     }
-    if constexpr (MORE) ring_use(add);
+    if constexpr (MORE) ring_use(add, forth);
     if constexpr (BWD) {
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
@@ -855,11 +859,11 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a)
     else held(std::false_type());
     copies_end();
     if constexpr (MORE) {
-      T* to = out + own_at + a.hold * row_step;
+      T* to = out + own_at + a.hold * row_step + ring_end;
       ring_use([&](const Raw<T, V>& v, const Raw<T, V>& g) {
         result(v, g, to);
-        to += row_step;
-      });
+        to -= row_step;
+      }, -forth);
     }
     if (++b == a.buffers) b = 0;
     turn ^= 1;
@@ -936,10 +940,14 @@ bool slice_lanes(int C, int cpg, int full, int* least, int* most) {
 constexpr int kHeldBytes = 92 * 1024;  // of shared memory per block, two on an SM
 
 // The held form.  Slices are 128 bytes of a pixel at least, where it has that many: at 64 the backward pass of 1904 images of 16x16x256 took 188 us,
-// at 128 145; at 32 the forward pass of 64 images of 224x224x64 608 us for 260 (other blocks read the rest of a line at other times).  Small
-// images: the smallest team (a warp to a block) that holds a slice in kPer pieces a thread, the slice as wide as that allows.  Larger ones: a
+// at 128 145; at 32 the forward pass of 64 images of 224x224x64 608 us for 260 (other blocks read the rest of a line at other times).  One or
+// two large images want more blocks than a cluster has, and their blocks run at the same time: narrower there (one image of 224x224x64 20 us in slices
+// of 128 bytes, 12.7 of 64, 10.1 of 32; four images 24, 23, 28).
+//   Small images: the smallest team (a warp to a block) that holds a slice in kPer pieces a thread, the slice as wide as that allows.  Larger ones: a
 // block, or as few blocks as give the SMs work, since blocks that exchange sums wait for one another (512 images of 28x28x128 forward: one
-// block 53 us, two 61, four 103, eight 190), even where the slice then does not fit; 64 images of 224x224x64: two 222 us, four 213, eight 209.
+// block 53 us, two 61, four 103, eight 190), even where the slice then does not fit.  But no more images are in work at a time than L2 keeps between
+// their two passes, as far as up to eight blocks to an image help that (256 images of 112x112x64 forward: one block 209 us, two 198, four 186,
+// eight 163, sixteen 201; 512 of 56x56x64 93, 85, 91, 113, 163; 64 of 224x224x64 319, 218, 212, 204, 215; backward 623, 387, 322, 332, 365).
 bool plan_held(int N, int P, int C, int cpg, int full, bool bwd, GnPlan* pl) {
   int least, most;
   if (!slice_lanes(C, cpg, full, &least, &most)) return false;
@@ -977,10 +985,16 @@ bool plan_held(int N, int P, int C, int cpg, int full, bool bwd, GnPlan* pl) {
     return true;
   }
   if (wide * full / cpg > 32) return false;
-  const long items = (long)N * (C / (wide * full)), slice = (long)P * wide * 16 * tensors;
+  int lanes = wide;
+  while (lanes > least && lanes > 2 && (long)N * (C / (lanes * full)) < 4) lanes /= 2;
+  const long items = (long)N * (C / (lanes * full)), slice = (long)P * lanes * 16 * tensors;
   int CS = 1;
-  while (CS < kMaxCluster && CS < P && slice / CS > 8192 && (items * CS < 128 || (items * CS < 256 && slice / CS > 4 * kHeldBytes))) CS *= 2;
-  fill(wide, kNT, CS);
+  while (CS < kMaxCluster && CS < P && slice / CS > 8192 && items * CS < 128) CS *= 2;
+  auto in_work = [&] { return (items < 296 / CS ? items : 296 / CS) * slice; };
+  while (CS < 8 && ((items * CS < 256 && slice / CS > 4 * kHeldBytes) ||
+                    (in_work() > 96l << 20 && (!bwd || CS < 4 || items >= 2 * (296 / (2 * CS))))))  // backward, eight blocks: not for a turn and a bit
+    CS *= 2;
+  fill(lanes, kNT, CS);
   return true;
 }
 
