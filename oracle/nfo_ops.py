@@ -1,4 +1,4 @@
-"""fp64 checker of the operators a step is composed from: group normalisation, linear layers, dropout, the 8-bit cache.
+"""fp64 oracle of the operators a step is composed from: group normalisation, linear layers, dropout, the 8-bit cache.
 
 Plain numpy in double precision, one function per formula, no code shared with the library.  Where an operator's definition itself
 rounds (the quantiser's fp32 scale and reciprocal, the dropout factor, the ReLU mask of group normalisation) the rounding is written out.

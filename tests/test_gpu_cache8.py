@@ -1,4 +1,4 @@
-"""The activation cache in 8 bits: codes, scales and read-back rows bit for bit against the checker."""
+"""The activation cache in 8 bits: codes, scales and read-back rows bit for bit against the oracle."""
 import numpy as np
 import pytest
 

@@ -1,4 +1,4 @@
-"""Dropout against the checker's generator: the same bits for every element, storage type and offset."""
+"""Dropout against the oracle's generator: the same bits for every element, storage type and offset."""
 import numpy as np
 import pytest
 

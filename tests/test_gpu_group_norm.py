@@ -1,4 +1,4 @@
-"""Group normalisation with its activation, forward and backward, against the fp64 checker.
+"""Group normalisation with its activation, forward and backward, against the fp64 oracle.
 
 Tolerances.  u = 2^-24.  A thread adds in fp32 what it sees of a group, at most 8 channels of the image's P pixels, then come a tree of 5 levels
 over lanes, up to 16 warps and the blocks' means: T = 8 P + 32 roundings at most.  What is added are distances from a value of the group

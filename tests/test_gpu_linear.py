@@ -1,4 +1,4 @@
-"""Linear layers and their gradients against the fp64 checker.
+"""Linear layers and their gradients against the fp64 oracle.
 
 Tolerances.  A sum of K products whose running value is rounded to fp32 (or cut off, in the tensor cores, at most once per 16 products and
 never coarser than 2^-23) is off by at most K u times the sum of the products' magnitudes, u = 2^-24, in whatever order it is taken; bias,
@@ -97,7 +97,7 @@ def test_gradients(env, si, dtype):
 
 
 def test_gradients_against_differences(env):
-    """f(x, w, b) = sum of dy * silu(x w^T + b + r): the chain of calls against central differences of the checker."""
+    """f(x, w, b) = sum of dy * silu(x w^T + b + r): the chain of calls against central differences of the oracle."""
     nf, torch = env
     M, K, N = 5, 12, 6
     r = np.random.default_rng(9)

@@ -72,7 +72,7 @@ class _Step:
         return {k: getattr(self, k).clone() for k in self.OUT}
 
     def want(self, step):
-        """The same in fp64 by autograd; the dropout mask and the cache's values from the checker."""
+        """The same in fp64 by autograd; the dropout mask and the cache's values from the oracle."""
         torch, F = self.torch, self.torch.nn.functional
         rows = oo.dequantize(self.codes.cpu().numpy().reshape(20, -1), self.scales.cpu().numpy(), "e4m3", 32)
         x = torch.from_numpy(rows.astype(np.float64)).view(20, self.H, self.H, self.C)[self.idx.cpu().long()].permute(0, 3, 1, 2)

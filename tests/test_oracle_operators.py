@@ -1,4 +1,4 @@
-"""Pins of the operators' fp64 checker: against autograd in double precision, finite differences, published test vectors and hand values."""
+"""Pins of the operators' fp64 oracle: against autograd in double precision, finite differences, published test vectors and hand values."""
 import numpy as np
 import pytest
 import torch
