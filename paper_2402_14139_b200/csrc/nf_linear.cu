@@ -110,14 +110,15 @@ __global__ void __launch_bounds__(256) gemm_join_kernel(const float* __restrict_
 // A few rows of x (MR at most) through weights contiguous along r: the weights are all the traffic.  A block of 128 threads takes kThinRows
 // weight rows; its threads share a row in 16-byte pieces, so that a block has 128 * kThinRows * 16 bytes on their way at a time, and each
 // piece of x serves kThinRows rows of weights.  Pairs of neighbouring products are added in one packed multiply-add; threads' sums meet by shuffles
-// and shared memory.  One row of 4096 x 8192 bf16 weights 13 us (5.2 TB/s).
+// and shared memory.  Rows that are not made of such pieces are read element by element.  One row of 4096 x 8192 bf16 weights 13 us (5.2 TB/s).
 constexpr int kThinRows = 4;
 // Up to four rows of bf16, 24 of fp32: beyond, the tensor cores take the product sooner (8 x 8192 x 4096 bf16 38 us here, 18 there; 32 x 2344 x 7416
 // fp32 64 us there, 24 rows 49 us here)
 template <typename T> constexpr int kThinMost = sizeof(T) == 4 ? 24 : 4;
 template <typename T> constexpr int kThinRowsOfX = sizeof(T) == 4 ? 8 : 4;  // of one block; more rows take the weights through L2 again
 
-template <typename T, int MR>
+// WHOLE: rows are made of 16-byte pieces; else a thread takes every 128th element, as many at a time
+template <typename T, int MR, bool WHOLE>
 __global__ void __launch_bounds__(128) thin_kernel(const T* __restrict__ x, const T* __restrict__ w, int M, int N, int K, const Epilogue e) {
   nf_pdl_begin();
   constexpr int V = 16 / sizeof(T), NP = V / 2;
@@ -128,8 +129,13 @@ __global__ void __launch_bounds__(128) thin_kernel(const T* __restrict__ x, cons
   for (int j = 0; j < kThinRows; ++j)
 #pragma unroll
     for (int m = 0; m < MR; ++m) acc[j][m] = 0;
-  auto pairs = [](const T* at, f32x2 (&v)[NP], bool stream) {
-    if constexpr (sizeof(T) == 2) {
+  auto pairs = [&](const T* row, int k, f32x2 (&v)[NP], bool stream) {
+    const T* at = row + k;
+    if constexpr (!WHOLE) {
+#pragma unroll
+      for (int i = 0; i < NP; ++i)
+        v[i] = nf_pack2(k + 256 * i < K ? ldf(at, 256 * i) : 0.f, k + 256 * i + 128 < K ? ldf(at, 256 * i + 128) : 0.f);
+    } else if constexpr (sizeof(T) == 2) {
       const uint4 u = stream ? __ldcs(reinterpret_cast<const uint4*>(at)) : __ldg(reinterpret_cast<const uint4*>(at));
       const uint32_t q[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
@@ -141,14 +147,14 @@ __global__ void __launch_bounds__(128) thin_kernel(const T* __restrict__ x, cons
     }
   };
 #pragma unroll 2
-  for (int k = threadIdx.x * V; k < K; k += 128 * V) {
+  for (int k = threadIdx.x * (WHOLE ? V : 1); k < K; k += 128 * V) {
     f32x2 b[kThinRows][NP];
 #pragma unroll
-    for (int j = 0; j < kThinRows; ++j) pairs(w + (size_t)min(n0 + j, N - 1) * K + k, b[j], true);  // rows beyond N: the last one again, not stored
+    for (int j = 0; j < kThinRows; ++j) pairs(w + (size_t)min(n0 + j, N - 1) * K, k, b[j], true);  // rows beyond N: the last one again, not stored
 #pragma unroll
     for (int m = 0; m < MR; ++m) {
       f32x2 a[NP];
-      pairs(x + (size_t)min(m0 + m, M - 1) * K + k, a, false);
+      pairs(x + (size_t)min(m0 + m, M - 1) * K, k, a, false);
 #pragma unroll
       for (int j = 0; j < kThinRows; ++j)
 #pragma unroll
@@ -173,10 +179,22 @@ __global__ void __launch_bounds__(128) thin_kernel(const T* __restrict__ x, cons
   }
 }
 
+// Where rows come in pieces, kThinMost of them, else one block's worth.  And any product whose blocks take no longer than the launches, pipeline and join
+// of the other kernels: each is about 3 ns at up to 512 long sums, 6 at 2000 (bf16 16 x 1024 x 1024 1024 blocks 5.6 us, 7.5 on the tensor cores;
+// 64 x 512 x 512 2048 blocks 8.1 and 6.1; 128 x 512 x 10 2.0 and 7.3; fp32 64 x 512 x 512 1024 blocks 6.8, 14 by the simple kernel, 64 x 1024 x 1024 2048
+// blocks 13.7 and 14.2; sums below 128, which that one does not split, 128 x 64 x 1024 4096 blocks 18.9 and 8.3).
 template <typename T>
+bool thin_pays(int P, int Q, int R) {
+  const bool half = sizeof(T) == 2;
+  if (P <= (R % (16 / (int)sizeof(T)) == 0 ? kThinMost<T> : kThinRowsOfX<T>)) return true;
+  const double blocks = (double)((Q + kThinRows - 1) / kThinRows) * ((P + kThinRowsOfX<T> - 1) / kThinRowsOfX<T>);
+  return blocks <= (half ? 1024 : R >= 128 ? 2048 : 512) && blocks * R <= (half ? 1 << 20 : 1 << 21);
+}
+
+template <typename T, bool WHOLE>
 int thin_product(const T* x, const T* w, int M, int N, int K, const Epilogue& e) {
   constexpr int most = kThinRowsOfX<T>;
-  auto k = M == 1 ? thin_kernel<T, 1> : M == 2 ? thin_kernel<T, 2> : M <= 4 ? thin_kernel<T, 4> : thin_kernel<T, most>;
+  auto k = M == 1 ? thin_kernel<T, 1, WHOLE> : M == 2 ? thin_kernel<T, 2, WHOLE> : M <= 4 ? thin_kernel<T, 4, WHOLE> : thin_kernel<T, most, WHOLE>;
   nf_launch(k, dim3((N + kThinRows - 1) / kThinRows, (M + most - 1) / most), 128, 0, x, w, M, N, K, e);
   NF_LAUNCHED();
   return NF_OK;
@@ -261,8 +279,16 @@ __global__ void __launch_bounds__(256) across_kernel(const T* __restrict__ A, co
   }
 }
 
+// Also any product short enough that the other kernels are waiting for launches, pipeline and join: fp32 up to 2^26 multiply-adds counted in whole columns of
+// blocks (256 x 256 x 256 5.4 us, 13.9 by the simple kernel; 64 x 1024 x 1024 12.3 and 13.9; 48 x 2344 x 7416 68 and 62 on the tensor cores), bf16 below
+// 2^24 (32 x 512 x 512 4.7 us, 5.6 on the tensor cores; 128 x 1000 x 100 4.2 and 7.0; at 2^24 256 x 256 x 256 6.3 and 5.3).
 template <typename T>
-bool across(int P, int Q) { return P <= kAcrossMost<T> && Q % (16 / (int)sizeof(T)) == 0; }
+bool across(int P, int Q, int R) {
+  constexpr int kCols = 512 / sizeof(T);
+  if (Q % (16 / (int)sizeof(T))) return false;
+  const double work = (double)P * (double)nf_align_up(Q, kCols) * R;
+  return P <= kAcrossMost<T> || (P <= 1 << 17 && (sizeof(T) == 4 ? work <= 67108864.0 : work < 16777216.0));
+}
 // Ranges of r: four blocks for each SM, 64 rows each at least and 4096 (512 steps of a running sum) at most
 template <typename T>
 int across_splits(int P, int Q, int R) {
@@ -589,7 +615,7 @@ bool on_tensor_cores(int dtype, const Product& d) {
   return dtype == NF_BF16 || (double)nf_align_up(d.P, 64) * (double)nf_align_up(d.Q, 64) * d.R >= 67108864.0;
 }
 bool few_across(int dtype, const Product& d) {
-  return d.a_along_r && !d.b_along_r && (dtype == NF_F32 ? across<float>(d.P, d.Q) : across<bf16>(d.P, d.Q));
+  return d.a_along_r && !d.b_along_r && (dtype == NF_F32 ? across<float>(d.P, d.Q, d.R) : across<bf16>(d.P, d.Q, d.R));
 }
 bool needs_copy(int dtype, int len) { return dtype == NF_F32 || len % 8; }
 size_t copy_bytes(int dtype, int rows, int len) {
@@ -663,8 +689,9 @@ int product(const Product& d, const void* A, const void* B, void* scratch, const
   const int dtype = sizeof(T) == 4 ? NF_F32 : NF_BF16;
   if ((d.Q + 63) / 64 > 65535) return NF_EUNSUPPORTED;
   if (d.a_along_r && d.R <= 64 && d.Q <= 64 && d.R * d.Q <= kRowsMost) return rows_product<T>((const T*)A, (const T*)B, d.P, d.Q, d.R, d.b_along_r, e);
-  if (d.P <= kThinMost<T> && d.a_along_r && d.b_along_r && d.R % (16 / (int)sizeof(T)) == 0)
-    return thin_product<T>((const T*)A, (const T*)B, d.P, d.Q, d.R, e);
+  if (d.a_along_r && d.b_along_r && thin_pays<T>(d.P, d.Q, d.R))
+    return d.R % (16 / (int)sizeof(T)) == 0 ? thin_product<T, true>((const T*)A, (const T*)B, d.P, d.Q, d.R, e)
+                                            : thin_product<T, false>((const T*)A, (const T*)B, d.P, d.Q, d.R, e);
   if (few_across(dtype, d)) return across_product<T>((const T*)A, (const T*)B, (float*)scratch, d, e);
   if (!d.a_along_r && !d.b_along_r && e.out_f32 && d.R <= kOuterMost<T> && d.Q % 4 == 0) return outer_product<T>((const T*)A, (const T*)B, d.P, d.Q, d.R, e);
   if constexpr (sizeof(T) == 4) {

@@ -26,6 +26,11 @@ SHAPES += [  # few rows forwards and backwards (whole and odd widths, sums cut i
     (16, 1028, 68), (17, 1028, 68), (12, 63, 77), (20000, 512, 10), (20000, 10, 512), (30000, 3, 600), (5, 20000, 36), (4, 36, 20000),
 ]
 
+SHAPES += [  # short products of any number of rows, on either side of what the kernels for few rows take
+    (30, 700, 701), (64, 256, 256), (64, 512, 512), (65, 1023, 40), (128, 1000, 100), (256, 256, 256), (1000, 512, 10), (5000, 128, 10), (100, 129, 1000),
+    (131072, 4, 68), (131073, 68, 2), (3, 3261, 1941), (8, 2001, 300), (9, 2001, 4097),
+]
+
 
 @pytest.fixture(scope="module")
 def env():
