@@ -556,7 +556,8 @@ __global__ void __launch_bounds__(256) act_backward_kernel(const T* saved, const
 }
 
 // Operand copies for the tensor cores: rows padded to 16 bytes, and fp32 cut into three bf16 parts whose sum is exact (each is the
-// nearest bf16 to what the earlier ones leave).  Memory bounds it; both operands in one launch: a product of 1777 x 2048 x 1000 64 -> 62 us, 318 x 840 x 2408 26.5 -> 24.9.
+// nearest bf16 to what the earlier ones leave).  Memory bounds it; both operands in one launch: a product of
+// 1777 x 2048 x 1000 62 us (64 in two), 318 x 840 x 2408 24.9 (26.5).
 struct PartsOf {
   const void* src;
   bf16* dst;
