@@ -802,7 +802,7 @@ extern "C" int nf_linear_wgrad(int dtype, const void* x, const void* g, int M, i
       nf_overlap(scratch, need, g, es * M * N))
     return NF_EINVAL;
   const SumPlan sums = sum_plan(M, N);
-  if (db && sums.cols > 65535) return NF_EUNSUPPORTED;
+  if (db && (N + 31) / 32 > 65535) return NF_EUNSUPPORTED;  // blocks along a row, where a thread has one column
   const Epilogue e{nullptr, nullptr, NF_ACT_NONE, nullptr, dw, 1};
   const Product d = wgrad_of(M, K, N);
   const int rc = dtype == NF_F32 ? product<float>(d, g, x, scratch, e) : product<bf16>(d, g, x, scratch, e);

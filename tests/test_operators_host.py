@@ -76,6 +76,8 @@ def test_refusals_of_sizes_and_of_scratch_in_use(nf):
         assert L.nf_linear_dgrad(1, far[0], far[1], m, k, n, far[2], 1 << 40, far[3]) == U
         assert L.nf_linear_wgrad(1, far[0], far[1], m, k, n, far[2], 1 << 40, far[3], None) == U
         assert L.nf_linear_scratch_bytes(1, m, k, n) == 0
+    for n in ((1 << 21) - 31, 1 << 23):                # bias gradients of more columns than a launch covers
+        assert L.nf_linear_wgrad(1, far[0], far[1], 4, 16, n, far[2], 1 << 40, far[3], far[4]) == U
     gsb, lsb = L.nf_group_norm_scratch_bytes(1, 2, 4, 16, 4), L.nf_linear_scratch_bytes(1, 4, 16, 8)
     for k in (0, 1, 2, 3, 7, 8, 9):
         assert L.nf_group_norm_backward(1, *A[:6], 2, 4, 16, 4, 1, A[k], gsb, *A[7:10]) == E, k
