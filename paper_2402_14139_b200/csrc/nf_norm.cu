@@ -15,9 +15,11 @@
 // special-function and FMA pipes with SiLU or GELU, whose derivative is taken in both passes (128 images of 32x32x128 backward 42 us, 2.4 TB/s),
 // and for images of several MB the second reading: 64 of 224x224x64 forward 205 us, of which L2 gives back a quarter of what is read twice.
 //
-// Sums: a thread adds in fp32 what it sees of its channels, in the forward pass after subtracting a value of the group or channel, so that a
-// mean far from zero costs no digits; ranges of pixels are joined by their means and squared deviations.  The gradient's ReLU mask is
-// decided on xh gamma + beta with every operation rounded by itself.
+// Sums of the forward pass: a thread takes its values in runs of a few dozen, subtracts the mean of what it has seen before (of its first few pixels
+// to begin with), and joins a run's mean and squared deviations to those of the runs before it; lanes, warps and blocks are joined in the same way.  So neither
+// a mean far from zero nor a value that is not like the others costs digits: in any run the squares added are at most about as large as the
+// deviations that come out.  The backward pass adds in fp32 what a thread sees, then in fp32 or fp64 over threads and blocks; its ReLU mask is decided on
+// xh gamma + beta with every operation rounded by itself.
 #include <cooperative_groups.h>
 
 #include <cuda.h>
@@ -126,6 +128,9 @@ __device__ __forceinline__ void store(T* p, const f32x2 (&v)[(V + 1) / 2]) {
   }
 }
 __device__ __forceinline__ f32x2 both(float v) { return nf_pack2(v, v); }
+// What is subtracted from values has to be finite: an infinity among them then gives the mean that it should
+__device__ __forceinline__ float finite_or_0(float v) { return fabsf(v) <= 3.4028234663852886e38f ? v : 0.f; }
+constexpr int kRun = 32;  // pixels of a thread between two joins of what it adds to its mean and squared deviations
 __device__ __forceinline__ float low(f32x2 v) { float a, b; nf_unpack2(v, a, b); return a; }
 __device__ __forceinline__ float high(f32x2 v) { float a, b; nf_unpack2(v, a, b); return b; }
 
@@ -218,8 +223,8 @@ __global__ void __launch_bounds__(kNT, V == 8 ? 2 : 4) group_norm_kernel(const G
   nf_pdl_begin();
   constexpr int NP = (V + 1) / 2, U = V < 8 || BWD ? 4 : 8;  // loads in flight per thread and tensor
   extern __shared__ __align__(16) float sm[];
-  float* red = sm;                        // [2V][kNT] tree reduction
-  float* tot = red + 2 * V * kNT;         // [2][2][Cs] this block's channel sums, two images in turn
+  float* red = sm;                        // [2V + 1][kNT] tree reduction
+  float* tot = red + (2 * V + 1) * kNT;   // [2][2][Cs] this block's channel sums (forward: means, squared deviations), two images in turn
   float* gsm = tot + 4 * a.Cs;            // [2][groups of the slice]: mean and rstd (forward), m1 and m2 (backward)
   float* acc = gsm + 2 * (a.Cs / a.cpg);  // backward: [2][Cs] sums over the images of this block
   cg::cluster_group cluster = cg::this_cluster();
@@ -248,20 +253,40 @@ __global__ void __launch_bounds__(kNT, V == 8 ? 2 : 4) group_norm_kernel(const G
     for (int cv0 = 0; cv0 < a.vpr; cv0 += cols) {
       const int cv = cv0 + tc;
       f32x2 s[NP], q[NP];
+      [[maybe_unused]] f32x2 mu[NP], m2[NP], nk[NP];  // forward: mean and squared deviations of the pixels seen, minus what is subtracted
+      [[maybe_unused]] float seen = 0.f;
 #pragma unroll
-      for (int i = 0; i < NP; ++i) s[i] = q[i] = 0;
+      for (int i = 0; i < NP; ++i) s[i] = q[i] = mu[i] = m2[i] = 0;
       if (on && cv < a.vpr) {
         const size_t col = base + (size_t)cv * V;
-        f32x2 nk[NP];  // forward: minus the pivots
         if constexpr (BWD) {
           if (!one_col) ch.affine(a, c0 + cv * V);
           ch.stats(cv * V, a.cpg, saved);
-        } else {
-          Raw<T, V> k;
-          k.load(x + col);
-#pragma unroll
-          for (int i = 0; i < NP; ++i) nk[i] = nf_mul2(k.pair(i), both(-1.f));
         }
+        auto subtract = [&](int i) { nk[i] = nf_pack2(-finite_or_0(low(mu[i])), -finite_or_0(high(mu[i]))); };
+        [[maybe_unused]] auto begin = [&](const Raw<T, V>* v, auto pixels) {  // the mean of the first pixels
+          constexpr int n = decltype(pixels)::value;
+#pragma unroll
+          for (int i = 0; i < NP; ++i) {
+#pragma unroll
+            for (int u = 0; u < n; ++u) mu[i] = nf_fma2(v[u].pair(i), both(1.f / n), mu[i]);
+            subtract(i);
+            mu[i] = nf_mul2(nk[i], both(-1.f));
+          }
+        };
+        [[maybe_unused]] auto join = [&](int pixels) {  // deviations from mu: new mean = mu + s / n, squared deviations from it + q - s^2 / n
+          const float n = seen + (float)pixels;
+          const f32x2 w = both(1.f / n);
+#pragma unroll
+          for (int i = 0; i < NP; ++i) {
+            const f32x2 d = nf_mul2(s[i], w);
+            m2[i] = nf_add2(m2[i], nf_fma2(nf_mul2(s[i], both(-1.f)), d, q[i]));
+            mu[i] = nf_add2(mu[i], d);
+            s[i] = q[i] = 0;
+            subtract(i);
+          }
+          seen = n;
+        };
         auto add = [&](const Raw<T, V>& v, const Raw<T, V>& g) {
 #pragma unroll
           for (int i = 0; i < NP; ++i) {
@@ -278,6 +303,8 @@ __global__ void __launch_bounds__(kNT, V == 8 ? 2 : 4) group_norm_kernel(const G
           }
         };
         int p = p0 + tr;
+        [[maybe_unused]] int run = 0;
+        [[maybe_unused]] bool begun = false;
         const size_t step = (size_t)R * a.C;
         size_t at = col + (size_t)p * a.C;
         for (; p + (U - 1) * R < p1; p += U * R, at += U * step) {
@@ -287,30 +314,66 @@ __global__ void __launch_bounds__(kNT, V == 8 ? 2 : 4) group_norm_kernel(const G
             v[u].load(x + at + u * step);
             if constexpr (BWD) g[u].load(dy + at + u * step);
           }
+          if constexpr (!BWD) {
+            if (!begun) begin(v, std::integral_constant<int, U>());
+            begun = true;
+          }
 #pragma unroll
           for (int u = 0; u < U; ++u) add(v[u], g[BWD ? u : 0]);
+          if constexpr (!BWD) {
+            if ((run += U) == kRun) {
+              join(run);
+              run = 0;
+            }
+          }
         }
         for (; p < p1; p += R, at += step) {
           Raw<T, V> v, g;
           v.load(x + at);
           if constexpr (BWD) g.load(dy + at);
           else g = v;
+          if constexpr (!BWD) {
+            if (!begun) begin(&v, std::integral_constant<int, 1>());
+            begun = true;
+            ++run;
+          }
           add(v, g);
+        }
+        if constexpr (!BWD) {
+          if (run) join(run);
         }
       }
       // rows of threads are folded in halves
       __syncthreads();
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        red[i * kNT + threadIdx.x] = i % 2 ? high(s[i / 2]) : low(s[i / 2]);
-        red[(V + i) * kNT + threadIdx.x] = i % 2 ? high(q[i / 2]) : low(q[i / 2]);
+        const f32x2 first = BWD ? s[i / 2] : mu[i / 2], second = BWD ? q[i / 2] : m2[i / 2];
+        red[i * kNT + threadIdx.x] = i % 2 ? high(first) : low(first);
+        red[(V + i) * kNT + threadIdx.x] = i % 2 ? high(second) : low(second);
       }
+      if constexpr (!BWD) red[2 * V * kNT + threadIdx.x] = seen;
       for (int left = R; left > 1;) {
         const int half = (left + 1) / 2;
         __syncthreads();
         if (tr + half < left) {
+          float* mine_at = red + threadIdx.x;
+          const float* other = mine_at + half * cols;
+          if constexpr (BWD) {
 #pragma unroll
-          for (int e = 0; e < 2 * V; ++e) red[e * kNT + threadIdx.x] += red[e * kNT + threadIdx.x + half * cols];
+            for (int e = 0; e < 2 * V; ++e) mine_at[e * kNT] += other[e * kNT];
+          } else {  // (count, mean, squared deviations) of both; rows further on never have more pixels
+            const float na = mine_at[2 * V * kNT], nb = other[2 * V * kNT];
+            if (nb > 0.f) {
+              const float w = __fdividef(nb, na + nb);  // two units in the last place are enough for a weight
+#pragma unroll
+              for (int e = 0; e < V; ++e) {
+                const float ma = mine_at[e * kNT], mb = other[e * kNT], base_m = finite_or_0(ma), d = mb - ma;
+                mine_at[e * kNT] = base_m + fmaf(mb - base_m, w, (ma - base_m) * (1.f - w));
+                mine_at[(V + e) * kNT] += other[(V + e) * kNT] + d * d * (na * w);
+              }
+              mine_at[2 * V * kNT] = na + nb;
+            }
+          }
         }
         left = half;
       }
@@ -326,24 +389,31 @@ __global__ void __launch_bounds__(kNT, V == 8 ? 2 : 4) group_norm_kernel(const G
     {
       int L = 1;
       while (L < a.cpg && L < 32) L *= 2;
+      [[maybe_unused]] const int cs_log = 31 - __clz(a.CS);
       const int lane = threadIdx.x % L, per = kNT / L;
       for (int g0 = 0; g0 < gps; g0 += per) {
         const int g = g0 + threadIdx.x / L;
-        double A = 0, B = 0;
+        double A = 0, B = 0, from = 0;  // forward: moments about the first channel's mean in the first block
         if (g < gps) {
+          if constexpr (!BWD) from = finite_or_0(cluster.map_shared_rank(mine, 0)[g * a.cpg]);
           for (int i = lane; i < a.cpg; i += L) {
             const int c = g * a.cpg + i;
             double S = 0, Q = 0;
 #pragma unroll 4
             for (int r = 0; r < a.CS; ++r) {
               const float* o = cluster.map_shared_rank(mine, r);
-              S += o[c];
-              Q += o[a.Cs + c];
+              if constexpr (BWD) {
+                S += o[c];
+                Q += o[a.Cs + c];
+              } else {  // CS is a power of two
+                const double n = (double)(int)(((long long)a.P * (r + 1) >> cs_log) - ((long long)a.P * r >> cs_log)), d = o[c] - from;
+                S += n * d;
+                Q += o[a.Cs + c] + n * d * d;
+              }
             }
-            if constexpr (!BWD) {  // mean and sum of squared deviations of the channel; the group's by their sums
-              const double d = S / a.P, m = (double)ldf(x, base + c) + d;
-              A += m;
-              B += Q / a.P - d * d + m * m;
+            if constexpr (!BWD) {
+              A += S / a.P;
+              B += Q / a.P;
             } else {
               const double gm = a.gamma[c0 + c];
               A += gm * S;
@@ -358,7 +428,7 @@ __global__ void __launch_bounds__(kNT, V == 8 ? 2 : 4) group_norm_kernel(const G
         if (g < gps && lane == 0) {
           if constexpr (!BWD) {
             const double m = A / a.cpg, var = B / a.cpg - m * m;
-            const float mf = (float)m, rf = (float)(1.0 / sqrt((var > 0 ? var : var == var ? 0 : var) + (double)a.eps));
+            const float mf = (float)(from + m), rf = (float)(1.0 / sqrt((var > 0 ? var : var == var ? 0 : var) + (double)a.eps));
             gsm[g] = mf;
             gsm[gps + g] = rf;
             if (rank == 0) {
@@ -446,8 +516,8 @@ __global__ void __launch_bounds__(kNT, V == 8 ? 2 : 4) group_norm_kernel(const G
 // A team of TS threads works on one image's slice (in a cluster: each block's team on a range of its pixels).  A slice is `vpr` 16-byte pieces
 // of a pixel, a power of two up to 32, whole groups; a thread takes pieces t, t + TS, ..., so its channels stay the same, and it alone
 // copies them into shared memory (cp.async), reads them in both passes and refills their places with the image `buffers` turns on: no
-// barrier guards the data.  Sums of a group: shuffles; teams of several warps add one number per warp and group through shared memory; blocks of a
-// cluster send theirs to each other (st.async into slots of the receiver, counted by its barrier).  FINE: groups of fewer channels than a piece;
+// barrier guards the data.  Sums of a group (forward: means and squared deviations): shuffles; teams of several warps join one pair per warp and group
+// through shared memory; blocks of a cluster send theirs to each other (st.async into slots of the receiver, counted by its barrier).  FINE: groups of fewer channels than a piece;
 // MORE: the slice is larger than what is held.
 constexpr int kSlotGroups = 64;
 
@@ -547,7 +617,8 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a)
     }
     copies_end();
   };
-  auto ring_use = [&](auto&& f, ptrdiff_t way) {  // f(x, dy) for each of this pass's pieces, way from one to the next
+  // f(x, dy) for each of this pass's pieces, way from one to the next; join(): kRun pieces have been used, in the first of those runs `before` fewer
+  auto ring_use = [&](auto&& f, ptrdiff_t way, int before, auto&& join) {
     auto step = [&](auto&& fill) {
       asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
       Raw<T, V> v, g;
@@ -570,6 +641,13 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a)
     const int same = ks - kRing;  // steps whose loads belong to this pass as well; the last of them is the pass's last load
     int k = 0;
     if (same > 1 && ring_n < a.N) {
+      if constexpr (!std::is_same<std::decay_t<decltype(join)>, std::nullptr_t>::value) {
+        for (int end = kRun - before; end <= same - 1; end += kRun) {
+#pragma unroll 4
+          for (; k < end; ++k) step(along);
+          join();
+        }
+      }
 #pragma unroll 4
       for (; k < same - 1; ++k) step(along);
       ring_left -= same - 1;
@@ -586,44 +664,83 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a)
 #pragma unroll
   for (int i = 0; i < NP; ++i) db[i] = dg[i] = 0;
 
-  // Read one image ahead: its statistics (backward), or the pivot of this thread's group, the group's first channel at the block's first pixel
-  float2 ahead = make_float2(0.f, 0.f);
-  const size_t pivot_at = (size_t)(p0 < a.P ? p0 : a.P - 1) * a.C + c0 + tc / lo * a.cpg;
+  // Backward: the statistics of this thread's group are read one image ahead
+  [[maybe_unused]] float2 ahead = make_float2(0.f, 0.f);
   auto look = [&](int n) {
-    if (FINE || n >= a.N) return;
-    if constexpr (BWD) {
-      const size_t g = (size_t)n * a.G + slice * gps + tc / lo;
-      ahead = make_float2(a.mean[g], a.rstd[g]);
-    } else {
-      ahead.x = ldf((const T*)a.x, (size_t)n * image + pivot_at);
-    }
+    if (!BWD || FINE || n >= a.N) return;
+    const size_t g = (size_t)n * a.G + slice * gps + tc / lo;
+    ahead = make_float2(a.mean[g], a.rstd[g]);
   };
+  // Forward: pixels that this thread sees, values that it and the warps of its team see of a group; runs count in `unit`s
+  const int own_px = whole + last, rest = np * a.vpr - whole * TS, pivots = min(kw + last_held, 4), from_lane = lane & (a.vpr - 1) & ~(lo - 1);
+  auto warp_values = [&](int w) { return (float)((32 * whole + min(max(rest - 32 * w, 0), 32)) / a.vpr * a.cpg); };
+  constexpr float unit = FINE ? 1.f : V;
+  const float own_n = (float)(own_px * (FINE ? a.cpg : V)), own_w = own_px ? 1.f / (own_px * unit) : 0.f;
+  const float warp_n = warp_values(t / 32), warp_w = warp_n > 0.f ? 1.f / warp_n : 0.f, pivot_w = pivots ? 1.f / (pivots * unit) : 0.f;
   look(first);
   int b = 0, turn = 0;
   uint32_t xph = 0;
   for (int n = first; n < a.N; n += a.stride) {
     const size_t gbase = (size_t)n * a.G + slice * gps;
     const uint32_t slot = slot0 + b * bstep;
-    f32x2 nk[BWD ? 1 : NS];
-    float pivot[S];
     if constexpr (BWD) {
       if constexpr (FINE) ch.stats(tc * V, a.cpg, [&](int i) { return make_float2(a.mean[gbase + i], a.rstd[gbase + i]); });
       else ch.stats(0, 1, [&](int) { return ahead; });
-    } else {
-      if constexpr (FINE) {
-        const T* px = (const T*)a.x + (size_t)n * image + (size_t)(p0 < a.P ? p0 : a.P - 1) * a.C + c0;
-#pragma unroll
-        for (int i = 0; i < V; ++i) pivot[i] = ldf(px, (tc * V + i) / a.cpg * a.cpg);
-      } else {
-        pivot[0] = ahead.x;
-      }
-#pragma unroll
-      for (int i = 0; i < NS; ++i) nk[i] = nf_pack2(-pivot[FINE ? 2 * i : 0], -pivot[FINE ? 2 * i + 1 : 0]);
     }
     look(n + a.stride);
     f32x2 s[NP], q[NP];
 #pragma unroll
     for (int i = 0; i < NP; ++i) s[i] = q[i] = 0;
+    // A thread's pairs added over the channels of each slot's group
+    auto slots = [&](const f32x2 (&from)[NP], float (&to)[S]) {
+      float v[V];
+#pragma unroll
+      for (int i = 0; i < NP; ++i) nf_unpack2(from[i], v[2 * i], v[2 * i + 1]);
+      if constexpr (FINE) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) to[i] = v[i];
+        // channels of a group lie next to each other in the thread
+        if (a.cpg >= 2) {
+#pragma unroll
+          for (int i = 0; i < S; i += 2) to[i] = to[i + 1 < S ? i + 1 : i] = to[i] + to[i + 1 < S ? i + 1 : i];
+        }
+        if (S == 8 && a.cpg >= 4) {
+#pragma unroll
+          for (int i = 0; i + 2 < S; i += 4) to[i] = to[i + 1] = to[i + 2] = to[i + 3] = to[i] + to[i + 2];
+        }
+      } else {
+        to[0] = v[0];
+#pragma unroll
+        for (int i = 1; i < V; ++i) to[0] += v[i];
+      }
+    };
+    // Forward: mean and squared deviations of what this thread has seen of its group, or FINE of each channel, and minus what is subtracted from
+    // the next values
+    [[maybe_unused]] float mu = 0.f, sq = 0.f;
+    [[maybe_unused]] f32x2 mu2[NP], sq2[NP], nk[NS];
+    auto subtract = [&] {
+#pragma unroll
+      for (int i = 0; i < NS; ++i)
+        nk[i] = FINE ? nf_pack2(-finite_or_0(low(mu2[i])), -finite_or_0(high(mu2[i]))) : both(-finite_or_0(mu));
+    };
+    // Deviations from that have been added: new mean = mu + s / n, squared deviations from it + q - s^2 / n.  w = 1 / n
+    auto join_run = [&](float w) {
+      if constexpr (FINE) {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+          sq2[i] = nf_add2(sq2[i], nf_fma2(nf_mul2(s[i], both(-w)), s[i], q[i]));
+          mu2[i] = nf_fma2(s[i], both(w), mu2[i]);
+        }
+      } else {
+        float f0[S], f1[S];
+        slots(s, f0);
+        slots(q, f1);
+        sq += fmaf(f0[0] * -w, f0[0], f1[0]);
+        mu = fmaf(f0[0], w, mu);
+      }
+#pragma unroll
+      for (int i = 0; i < NP; ++i) s[i] = q[i] = 0;
+    };
     auto add = [&](const Raw<T, V>& v, const Raw<T, V>& g) {
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
@@ -656,13 +773,64 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a)
       };
       uint32_t at = slot;
       int k = kw;
+      if constexpr (!BWD) {  // what is subtracted to begin with: the mean of the first four pieces
+        f32x2 sum[NP];
+#pragma unroll
+        for (int i = 0; i < NP; ++i) sum[i] = sq2[i] = 0;
+        auto more = [&](const Raw<T, V>& v) {
+#pragma unroll
+          for (int i = 0; i < NP; ++i) sum[i] = nf_fma2(v.pair(i), both(pivot_w), sum[i]);
+        };
+        auto begin = [&] {
+          if constexpr (!FINE) {
+            float m[S];
+            slots(sum, m);
+            mu = finite_or_0(m[0]);
+          } else {
+#pragma unroll
+            for (int i = 0; i < NP; ++i) mu2[i] = nf_pack2(finite_or_0(low(sum[i])), finite_or_0(high(sum[i])));
+          }
+          subtract();
+        };
+        if (kw >= 4) {
+          Raw<T, V> v[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) v[u].load_shared(slot + u * kstep);
+#pragma unroll
+          for (int u = 0; u < 4; ++u) more(v[u]);
+          begin();
+#pragma unroll
+          for (int u = 0; u < 4; ++u) add(v[u], v[u]);
+          at += 4 * kstep;
+          k -= 4;
+        } else {
+          for (int u = 0; u < pivots; ++u) {
+            Raw<T, V> v;
+            v.load_shared(slot + u * kstep);
+            more(v);
+          }
+          begin();
+        }
+      }
       for (; k >= 4; k -= 4, at += 4 * kstep) {
 #pragma unroll
         for (int u = 0; u < 4; ++u) one(at + u * kstep);
       }
       for (k += last_held; k > 0; --k, at += kstep) one(at);
     }
-    if constexpr (MORE) ring_use(add, forth);
+    if constexpr (!BWD) {
+      if constexpr (MORE) {
+        float seen = 0.f;
+        ring_use(add, forth, kw, [&] {
+          seen += kRun * unit;
+          join_run(1.f / seen);
+          subtract();
+        });
+      }
+      join_run(own_w);
+    } else if constexpr (MORE) {
+      ring_use(add, forth, 0, nullptr);
+    }
     if constexpr (BWD) {
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
@@ -672,47 +840,70 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a)
         q[i] = nf_mul2(q[i], ch.ga[i]);
       }
     }
-    float f[2][S];
+    // Over the lanes that share the group, all values side by side: shuffles stay in order, and each waits for the one before it of its own value only.
+    // Forward, FINE: a group's first channel stands for it
+    auto over_lanes = [&](auto& v) {
+      constexpr int n = sizeof(v) / sizeof(float);
+      float* w = reinterpret_cast<float*>(&v);
 #pragma unroll
-    for (int w = 0; w < 2; ++w) {
-      float v[V];
+      for (int o = 1; o < 32; o *= 2)
+        if (o < lo || o >= a.vpr) {
 #pragma unroll
-      for (int i = 0; i < NP; ++i) nf_unpack2(w ? q[i] : s[i], v[2 * i], v[2 * i + 1]);
+          for (int i = 0; i < n; ++i)
+            if (BWD || !FINE || !(i & (a.cpg - 1))) w[i] += __shfl_xor_sync(0xffffffffu, w[i], o);
+        }
+    };
+    float f[2][S];  // backward: sums; forward: mean and squared deviations
+    if constexpr (BWD) {
+      slots(s, f[0]);
+      slots(q, f[1]);
+      over_lanes(f);
+    } else {
+      if constexpr (FINE) {  // channels of a group: as many pixels of each
+        f32x2 v[NP];
+        const f32x2 w = both(1.f / a.cpg), px = both((float)own_px);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) v[i] = nf_mul2(mu2[i], w);
+        slots(v, f[0]);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+          const f32x2 d = nf_add2(mu2[i], nf_pack2(-f[0][2 * i], -f[0][S > 1 ? 2 * i + 1 : 0]));
+          v[i] = nf_fma2(nf_mul2(d, px), d, sq2[i]);
+        }
+        slots(v, f[1]);
+      } else {
+        f[0][0] = mu;
+        f[1][0] = sq;
+      }
+      float m[S], from[S];
+#pragma unroll
+      for (int i = 0; i < S; ++i) {
+        from[i] = finite_or_0(__shfl_sync(0xffffffffu, f[0][i], from_lane));  // no lane of the group has more pixels
+        m[i] = own_n * (f[0][i] - from[i]);
+      }
+      over_lanes(m);
+#pragma unroll
+      for (int i = 0; i < S; ++i) {
+        m[i] = fmaf(m[i], warp_w, from[i]);
+        const float d = f[0][i] - m[i];
+        f[0][i] = m[i];
+        f[1][i] = own_px ? fmaf(own_n * d, d, f[1][i]) : 0.f;
+      }
+      over_lanes(f[1]);
+#pragma unroll
+      for (int i = 0; i < S; ++i) f[1][i] = f[1][i] < 0.f ? 0.f : f[1][i];  // a NaN stays one
       if constexpr (FINE) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) f[w][i] = v[i];
-        // channels of a group lie next to each other in the thread
-        if (a.cpg >= 2) {
+        for (int w = 0; w < 2; ++w) {
 #pragma unroll
-          for (int i = 0; i < S; i += 2) f[w][i] = f[w][i + 1 < S ? i + 1 : i] = f[w][i] + f[w][i + 1 < S ? i + 1 : i];
+          for (int i = 1; i < S; ++i) {
+            if (i % 2 && a.cpg >= 2) f[w][i] = f[w][i - 1];
+            if (i % 4 == 2 && a.cpg >= 4) f[w][i] = f[w][i - 2];
+          }
         }
-        if (S == 8 && a.cpg >= 4) {
-#pragma unroll
-          for (int i = 0; i + 2 < S; i += 4) f[w][i] = f[w][i + 1] = f[w][i + 2] = f[w][i + 3] = f[w][i] + f[w][i + 2];
-        }
-      } else {
-        f[w][0] = v[0];
-#pragma unroll
-        for (int i = 1; i < V; ++i) f[w][0] += v[i];
       }
     }
-    // over the lanes that share the group
-#pragma unroll
-    for (int o = 1; o < 32; o *= 2)
-      if (o < lo || o >= a.vpr) {
-#pragma unroll
-        for (int w = 0; w < 2; ++w)
-#pragma unroll
-          for (int i = 0; i < S; ++i) f[w][i] += __shfl_xor_sync(0xffffffffu, f[w][i], o);
-      }
     const float M = (float)a.P * a.cpg;
-    // Group totals (A, B) of a block's pixels -> mean, squared deviations; statistics -> what pass two wants
-    auto about = [&](float& A, float& B, float k, int pixels) {
-      const float d = pixels ? A / ((float)pixels * a.cpg) : 0.f;
-      B = fmaf(-A, d, B);
-      if (B < 0.f) B = 0.f;  // a NaN stays one
-      A = k + d;
-    };
     float2 mine[S];
     if (warps == 1) {
 #pragma unroll
@@ -720,7 +911,6 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a)
         if constexpr (BWD) {
           mine[i] = make_float2(-f[0][i] / M, -f[1][i] / M);
         } else {
-          about(f[0][i], f[1][i], pivot[i], np);
           mine[i] = make_float2(f[0][i], 1.f / sqrtf(f[1][i] / M + a.eps));
         }
       }
@@ -747,14 +937,26 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a)
       float2* own = gsm + team * warps * 32;  // up to 32 groups per warp of the team
       // a warp per group: its lanes join the warps' sums (A in the lower half, B in the upper), then the other blocks'
       for (int g = t / 32; g < gps; g += warps) {
-        const int w = lane & 15;
-        float v = w < warps ? part[team * warps + w][lane >> 4][g] : 0.f;
-        float k = 0.f;
-        if constexpr (!BWD) k = ldf((const T*)a.x, (size_t)n * image + (size_t)(p0 < a.P ? p0 : a.P - 1) * a.C + c0 + g * a.cpg);
+        float A, B;
+        if constexpr (BWD) {
+          const int w = lane & 15;
+          float v = w < warps ? part[team * warps + w][lane >> 4][g] : 0.f;
 #pragma unroll
-        for (int o = 1; o < 16; o *= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
-        float A = __shfl_sync(0xffffffffu, v, 0), B = __shfl_sync(0xffffffffu, v, 16);
-        if constexpr (!BWD) about(A, B, k, np);
+          for (int o = 1; o < 16; o *= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
+          A = __shfl_sync(0xffffffffu, v, 0);
+          B = __shfl_sync(0xffffffffu, v, 16);
+        } else {
+          const float wn = lane < warps ? warp_values(lane) : 0.f, wm = wn > 0.f ? part[team * warps + lane][0][g] : 0.f;
+          const float from = finite_or_0(__shfl_sync(0xffffffffu, wm, 0));  // no warp has more pixels than the first
+          A = wn > 0.f ? wn * (wm - from) : 0.f;
+#pragma unroll
+          for (int o = 1; o < NT / 32; o *= 2) A += __shfl_xor_sync(0xffffffffu, A, o);
+          A = from + (np ? __shfl_sync(0xffffffffu, A, 0) / ((float)np * a.cpg) : 0.f);
+          B = wn > 0.f ? fmaf(wn * (wm - A), wm - A, part[team * warps + lane][1][g]) : 0.f;
+#pragma unroll
+          for (int o = 1; o < NT / 32; o *= 2) B += __shfl_xor_sync(0xffffffffu, B, o);
+          B = __shfl_sync(0xffffffffu, B, 0);
+        }
         if (a.CS > 1) {
           if (t == 0 && g == 0) ptx::mbar_expect_tx(&xbar[turn], a.CS * gps * 8);  // once: the barrier counts one arrival
           if (lane < a.CS) ptx::st_async_f2(&peers[turn][rank][g], A, B, &xbar[turn], lane);
@@ -768,7 +970,7 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a)
           if (g == t / 32) ptx::mbar_wait(&xbar[turn], (xph >> turn) & 1, &abort_word);  // sets the abort word itself when it gives up
           const float2 from = lane < a.CS ? peers[turn][lane][g] : make_float2(0.f, 0.f);
           const float cr = lane < a.CS ? (float)max(0, min(a.P - lane * a.rpc, a.rpc)) : 0.f;
-          const float base = __shfl_sync(0xffffffffu, from.x, 0);  // block 0 has pixels: means are joined by their distances from its mean
+          const float base = finite_or_0(__shfl_sync(0xffffffffu, from.x, 0));  // block 0 has pixels: means are joined by their distances from its mean
           const float d = BWD ? from.x : cr > 0.f ? from.x - base : 0.f;
           float m = BWD ? d : cr * d, M2 = from.y;
 #pragma unroll
@@ -867,7 +1069,7 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a)
       ring_use([&](const Raw<T, V>& v, const Raw<T, V>& g) {
         result(v, g, to);
         to -= row_step;
-      }, -forth);
+      }, -forth, 0, nullptr);
     }
     if (++b == a.buffers) b = 0;
     turn ^= 1;
@@ -1032,7 +1234,7 @@ GnPlan plan_gn(int dtype, int N, int P, int C, int groups, bool bwd) {
   pl.stride = (int)most;
   pl.rows = (int)most * pl.CS;
   const int Cs = C / pl.slices;
-  pl.smem = sizeof(float) * ((size_t)2 * pl.V * kNT + 4 * Cs + 2 * (Cs / cpg) + (bwd ? 2 * Cs : 0));
+  pl.smem = sizeof(float) * ((size_t)(2 * pl.V + 1) * kNT + 4 * Cs + 2 * (Cs / cpg) + (bwd ? 2 * Cs : 0));
   return pl;
 }
 
