@@ -354,7 +354,8 @@ int nf_group_norm_backward(int dtype, const void* x, const void* dy, const float
  *                    be dy's or saved's memory.  Not needed without an activation: then g = dy.
  *   nf_linear_dgrad: dx = g w [M][K].
  *   nf_linear_wgrad: dw = g^T x, float [N][K]; db = column sums of g, float [N], or NULL.
- * All but nf_act_backward need nf_linear_scratch_bytes() of scratch (overwritten).  fp32 operands have to be finite and below 2^127 in
+ * All but nf_act_backward need nf_linear_scratch_bytes() of scratch (overwritten).  Sums are held in fp32, in runs of at most 1024 products where the
+ * tensor cores, which cut a running sum off instead of rounding it, add them.  fp32 operands have to be finite and below 2^127 in
  * magnitude: an infinity among them may give NaN instead of an infinity; operands below 2^-102 may lose digits.  NF_EINVAL: sizes < 1; NF_EUNSUPPORTED: sizes
  * above 2^30, results of more than 2^22 - 64 columns (N forward, K of dx and dw), db of more than 2^21 - 32. */
 int nf_linear_forward(int dtype, const void* x, const void* w, const float* bias, const void* residual, int M, int K, int N, int act, void* scratch,

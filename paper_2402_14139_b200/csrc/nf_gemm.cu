@@ -6,9 +6,10 @@
 // out of tensor memory (two sets, so the next tile's products go on) through shared memory to TMA stores.  Operands are read
 // as they lie: contiguous along r (K-major) or along p / q (MN-major), so that no transposed copy exists.
 //
-// fp32 results: the tensor core cuts low bits off its running sum at every instruction, always towards zero (about 2^-25 of it here), so
-// a sum over thousands of products would lose the digits that fp32 has.  Accumulators then change every `seg` steps of 64 and
-// the warps add them up in registers.  fp32 operands come as three bf16 parts, x = h + m + l exactly, and the six products
+// The tensor core cuts low bits off its running sum at every instruction, always towards zero (about 2^-25 of it here), so a sum over
+// thousands of products would lose the digits that fp32 has, and one over 2^18 of one sign a third of a bf16 step (1.5e-3 of the result).  Accumulators
+// therefore change every `seg` steps of 64 and the warps add them up in registers: every 8 steps (3 of parts) for fp32 results, every 16 for bf16 ones,
+// which bounds their loss at 2^-18 whatever the length (358 us instead of 354 for the input gradient of 8602 x 8192 -> 4096; sums up to 1024 need it not).  fp32 operands come as three bf16 parts, x = h + m + l exactly, and the six products
 // l h, h l, m m, h m, m h, h h; what is left out is below 2^-24 of |x| |w|.  The three parts of a step of 64 lie in three stages side by side,
 // so that each is brought in once for all its products.
 //
@@ -28,6 +29,7 @@ namespace {
 
 constexpr int kGemmThreads = 320;  // warp 0: TMA, warp 1: products, warps 2-9: epilogue
 constexpr int kBox = 64;           // r per operand tile: 128 bytes of bf16
+constexpr int kSegBf16 = 16;       // bf16 results: operand tiles between two readings of an accumulator
 // Tiles of 32 rows x 128 bytes per epilogue warp on their way out: two, or one where sums are long (fp32 results) and a sixth operand stage
 // is worth more: the parts of the next step of 64 are then all on their way while this one's are multiplied
 template <typename T> constexpr int kTiles = sizeof(T) == 4 ? 1 : 2;
@@ -230,11 +232,11 @@ struct WayOut {
 template <int CG, int BN, typename T> constexpr int kGemmStages = (227 * 1024 - 1024 - 512 - kStaging<T>) / (128 * 128 + BN / CG * 128);
 template <int CG, int BN, typename T> constexpr int kGemmSmem = 1024 + kGemmStages<CG, BN, T> * (128 * 128 + BN / CG * 128) + kStaging<T> + 512;
 
-template <int CG, int BN, typename T>
+// SEG: the accumulators change every p.seg steps of 64, and the warps add them up in registers
+template <int CG, int BN, typename T, bool SEG>
 __global__ void __launch_bounds__(kGemmThreads, 1)
 gemm_tc_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const __grid_constant__ CUtensorMap tm_c,
                const __grid_constant__ CUtensorMap tm_r, const __grid_constant__ CUtensorMap tm_p, const __grid_constant__ GemmParams p) {
-  constexpr bool kSegments = sizeof(T) == 4;
   constexpr int kStages = kGemmStages<CG, BN, T>, kA = 128 * 128, kB = BN / CG * 128, kStage = kA + kB;
   constexpr uint32_t kCols = 2 * BN;
   extern __shared__ uint8_t smem_raw[];
@@ -336,7 +338,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
         unit_at(p, u, pt, qt, sp);
         k_range(sp, k0, k1);
         for (int kb = k0; ok && kb < k1;) {
-          const int end = kSegments ? (kb + p.seg < k1 ? kb + p.seg : k1) : k1;
+          const int end = SEG ? (kb + p.seg < k1 ? kb + p.seg : k1) : k1;
           if (!ptx::mbar_wait(&tempty[acc], aph ^ 1, abort_flag)) { ok = false; break; }
           ptx::tc_fence_after();
           const uint32_t d = tmem + acc * BN;
@@ -348,7 +350,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
               add = 1;
             }
           };
-          if (kSegments && p.planes == 3) {  // parts l, m, h in three stages, each given back after its last use, in the order they are filled again
+          if (SEG && p.planes == 3) {  // parts l, m, h in three stages, each given back after its last use, in the order they are filled again
             for (; ok && kb < end; kb += 3) {
               uint32_t st[3], at[3];
 #pragma unroll
@@ -406,7 +408,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__
       const int row0 = pt * 128 * CG + (int)rank * 128 + lg * 32, col0 = qt * BN + half * (BN / 2);
       const uint32_t taddr = tmem + ((uint32_t)(lg * 32) << 16) + half * (BN / 2);
       out.fetch(p, &tm_r, out.turn & (kTiles<T> - 1), row0, col0);
-      if constexpr (kSegments) {
+      if constexpr (SEG) {
         float sum[BN / 2];
 #pragma unroll
         for (int i = 0; i < BN / 2; ++i) sum[i] = 0.f;
@@ -479,7 +481,7 @@ int make_map3(CUtensorMap* m, const void* base, bool f32, size_t inner, size_t o
   return nf_tc_map3(m, base, f32, inner, outer, planes, ld * es, (planes > 1 ? plane : ld * outer) * es, rows);
 }
 
-template <int CG, int BN, typename T>
+template <int CG, int BN, typename T, bool SEG>
 int launch(const GemmProblem& g, const Epilogue& e, float* part, int splits) {
   GemmParams p{};
   p.P = g.P;
@@ -491,7 +493,7 @@ int launch(const GemmProblem& g, const Epilogue& e, float* part, int splits) {
   p.splits = splits;
   // 24 products of 16 (fp32 by parts), or 32, between two readings of an accumulator: errors of 1.6e-7 and 3e-7, the running sum losing about 2^-25 of
   // itself at each.  Twice as many cost fp32 6.6e-7 for 60 us instead of 64 (1777 x 2048 x 1000).
-  p.seg = p.planes == 3 ? 3 : 8;
+  p.seg = p.planes == 3 ? 3 : sizeof(T) == 4 ? 8 : kSegBf16;
   p.a_along_r = g.A.along_r;
   p.b_along_r = g.B.along_r;
   p.e = e;
@@ -520,7 +522,7 @@ int launch(const GemmProblem& g, const Epilogue& e, float* part, int splits) {
   int dev = 0;
   NF_CUDA(cudaGetDevice(&dev));
   if (dev < 0 || dev >= 64) return NF_EUNSUPPORTED;
-  auto k = gemm_tc_kernel<CG, BN, T>;
+  auto k = gemm_tc_kernel<CG, BN, T, SEG>;
   if (!ready[dev]) {
     NF_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmem<CG, BN, T>));
     ready[dev] = true;
@@ -551,6 +553,8 @@ int nf_gemm_tc(const GemmProblem& g, const Epilogue& e, float* part) {
   const int splits = nf_gemm_splits(g.P, g.Q, g.R, g.planes);
   if (tiles * splits > 0x3fffffffl) return NF_EUNSUPPORTED;
   const bool f32 = g.out_f32 || splits > 1;
-  if (large_tiles(g.P, g.Q)) return f32 ? launch<2, 256, float>(g, e, part, 1) : launch<2, 256, bf16>(g, e, part, 1);
-  return f32 ? launch<1, 128, float>(g, e, part, splits) : launch<1, 128, bf16>(g, e, part, splits);
+  const bool large = large_tiles(g.P, g.Q), seg = (g.R + kBox - 1) / kBox > kSegBf16;
+  if (f32) return large ? launch<2, 256, float, true>(g, e, part, 1) : launch<1, 128, float, true>(g, e, part, splits);
+  if (seg) return large ? launch<2, 256, bf16, true>(g, e, part, 1) : launch<1, 128, bf16, true>(g, e, part, splits);
+  return large ? launch<2, 256, bf16, false>(g, e, part, 1) : launch<1, 128, bf16, false>(g, e, part, splits);
 }
