@@ -599,6 +599,13 @@ def _choice(what, table, key):
     return table[key]
 
 
+def _group(group):
+    """Checked here as well as in the library: the shape of the scales follows from it, and a C int keeps its low 32 bits only."""
+    if group != 32 and group != 64 and group != 128:
+        raise NfError(f"group: 32, 64 or 128, not {group!r}")
+    return group
+
+
 def _scratch(t, dev):
     return _tensor("scratch", t, _TYPES["u8"], t.shape, dev), t.numel()
 
@@ -621,7 +628,7 @@ def nf_group_norm_forward(dtype, x, gamma, beta, groups, eps, act, y, mean, rstd
     """y = act(group_norm(x)): x, y [N, ..., C] of dtype (all dimensions between are pixels), gamma, beta float32 [C], act a key of
     ACTS; mean, rstd float32 [N, groups] are written for the backward pass."""
     N, P, C_ = _images(x)
-    td, f32, dev = _call(dtype, N, P, C_)
+    td, f32, dev = _call(dtype, N, P, C_, groups)
     _check(lib().nf_group_norm_forward(dtype, _tensor("x", x, td, x.shape, dev), _tensor("gamma", gamma, f32, (C_,), dev),
                                        _tensor("beta", beta, f32, (C_,), dev), N, P, C_, groups, eps, _choice("act", ACTS, act),
                                        _tensor("y", y, td, x.shape, dev), _tensor("mean", mean, f32, (N, groups), dev),
@@ -636,8 +643,8 @@ def nf_group_norm_backward(dtype, x, dy, gamma, beta, mean, rstd, act, scratch, 
     """dx, dgamma, dbeta from x, dy and what the forward pass left in mean and rstd [N, groups]; scratch: uint8 tensor of at least
     nf_group_norm_scratch_bytes(dtype, N, P, C, groups)."""
     N, P, C_ = _images(x)
-    td, f32, dev = _call(dtype, N, P, C_)
     groups, c = _matrix("mean", mean)[1], (C_,)
+    td, f32, dev = _call(dtype, N, P, C_, groups)
     _check(lib().nf_group_norm_backward(dtype, _tensor("x", x, td, x.shape, dev), _tensor("dy", dy, td, x.shape, dev),
                                         _tensor("gamma", gamma, f32, c, dev), _tensor("beta", beta, f32, c, dev),
                                         _tensor("mean", mean, f32, (N, groups), dev), _tensor("rstd", rstd, f32, (N, groups), dev), N, P, C_, groups,
@@ -699,9 +706,9 @@ def nf_cache_quantize(fmt, dtype, x, group, codes, scales):
     rows = x.shape[0]
     td, f32, dev = _call(dtype, rows)
     E = x.numel() // (rows or 1)
-    _check(lib().nf_cache_quantize(_choice("format", CACHE_FORMATS, fmt), dtype, _tensor("x", x, td, x.shape, dev), rows, E, group,
+    _check(lib().nf_cache_quantize(_choice("format", CACHE_FORMATS, fmt), dtype, _tensor("x", x, td, x.shape, dev), rows, E, _group(group),
                                    _tensor("codes", codes, _TYPES["u8"], x.shape, dev),
-                                   _tensor("scales", scales, f32, (rows, -(-E // (group or 1))), dev)), "nf_cache_quantize")
+                                   _tensor("scales", scales, f32, (rows, -(-E // group)), dev)), "nf_cache_quantize")
 
 
 def nf_cache_gather_quantized(fmt, codes, scales, cache_labels, idx, group, dtype, out, out_labels):
@@ -709,10 +716,10 @@ def nf_cache_gather_quantized(fmt, codes, scales, cache_labels, idx, group, dtyp
     cache_labels may lie in pinned host memory; idx int32.  Indices outside the cache as in nf_cache_gather."""
     rows, count = codes.shape[0], idx.numel()
     td, f32, dev = _call(dtype, rows, count)
-    E, i32 = codes.numel() // (rows or 1), _TYPES["i32"]
+    E, i32, group = codes.numel() // (rows or 1), _TYPES["i32"], _group(group)
     _check(lib().nf_cache_gather_quantized(
         _choice("format", CACHE_FORMATS, fmt), _tensor("codes", codes, _TYPES["u8"], codes.shape, dev, True),
-        _tensor("scales", scales, f32, (rows, -(-E // (group or 1))), dev, True),
+        _tensor("scales", scales, f32, (rows, -(-E // group)), dev, True),
         None if cache_labels is None else _tensor("cache_labels", cache_labels, i32, (rows,), dev, True), rows, _tensor("idx", idx, i32, (count,), dev),
         count, E, group, dtype, _tensor("out", out, td, (count,) + codes.shape[1:], dev), _maybe("out_labels", out_labels, i32, (count,), dev)),
         "nf_cache_gather_quantized")
