@@ -5,6 +5,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <initializer_list>
+
 #include "../../include/nf.h"
 
 typedef __nv_bfloat16 bf16;
@@ -158,6 +160,20 @@ static inline size_t nf_align_up(size_t v, size_t a) { return (v + a - 1) / a * 
 static inline size_t nf_esize(int dtype) { return dtype == NF_F32 ? 4 : 2; }
 static inline bool nf_overlap(const void* a, size_t na, const void* b, size_t nb) {
   return a && b && (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+}
+// Whether something written shares memory with something read or with something else written; absent tensors are NULL
+struct nf_extent {
+  const void* at;
+  size_t bytes;
+};
+static inline bool nf_shared(std::initializer_list<nf_extent> written, std::initializer_list<nf_extent> read) {
+  for (const nf_extent* w = written.begin(); w != written.end(); ++w) {
+    for (const nf_extent* o = w + 1; o != written.end(); ++o)
+      if (nf_overlap(w->at, w->bytes, o->at, o->bytes)) return true;
+    for (const nf_extent& r : read)
+      if (nf_overlap(w->at, w->bytes, r.at, r.bytes)) return true;
+  }
+  return false;
 }
 
 // ---- generic CUDA-core kernels (nf_direct.cu, nf_elem.cu): any shape, fp32 or bf16 storage, fp32 accumulate

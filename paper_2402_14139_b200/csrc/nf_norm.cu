@@ -24,8 +24,6 @@
 
 #include <cuda.h>
 
-#include <initializer_list>
-
 #include "nf_act.cuh"
 #include "nf_ldst.cuh"
 #include "nf_ptx.cuh"
@@ -1351,8 +1349,8 @@ extern "C" int nf_group_norm_forward(int dtype, const void* x, const float* gamm
   if (!x || !gamma || !beta || !y || !mean || !rstd || !gn_args_ok(dtype, N, P, C, groups) || !nf_act_ok(act) || !(eps > 0.f)) return NF_EINVAL;
   if (((uintptr_t)x | (uintptr_t)gamma | (uintptr_t)beta | (uintptr_t)y | (uintptr_t)mean | (uintptr_t)rstd) & 15) return NF_EALIGN;
   if (!gn_size_ok(N, P, C, groups)) return NF_EUNSUPPORTED;
-  const size_t bytes = (size_t)N * P * C * nf_esize(dtype);
-  if (nf_overlap(x, bytes, y, bytes)) return NF_EINVAL;
+  const size_t bytes = (size_t)N * P * C * nf_esize(dtype), cb = (size_t)C * 4, sb = (size_t)N * groups * 4;
+  if (nf_shared({{y, bytes}, {mean, sb}, {rstd, sb}}, {{x, bytes}, {gamma, cb}, {beta, cb}})) return NF_EINVAL;
   GnPlan pl = plan_gn(dtype, N, P, C, groups, false);
   GnArgs a{};
   if (fill_gn(a, pl, N, P, C, groups, act) != NF_OK) return NF_ECUDA;
@@ -1378,12 +1376,9 @@ extern "C" int nf_group_norm_backward(int dtype, const void* x, const void* dy, 
   const size_t bytes = (size_t)N * P * C * nf_esize(dtype);
   GnPlan pl = plan_gn(dtype, N, P, C, groups, true);
   if (scratch_bytes < (size_t)pl.rows * 2 * C * sizeof(float)) return NF_ENOWS;
-  const size_t used = (size_t)pl.rows * 2 * C * sizeof(float);
-  if (nf_overlap(x, bytes, dx, bytes) || nf_overlap(dy, bytes, dx, bytes)) return NF_EINVAL;
-  for (const void* t : {x, dy, (const void*)dx})
-    if (nf_overlap(scratch, used, t, bytes)) return NF_EINVAL;
-  for (const void* t : {(const void*)dgamma, (const void*)dbeta, (const void*)gamma, (const void*)beta})
-    if (nf_overlap(scratch, used, t, (size_t)C * 4)) return NF_EINVAL;
+  const size_t used = (size_t)pl.rows * 2 * C * sizeof(float), cb = (size_t)C * 4, sb = (size_t)N * groups * 4;
+  if (nf_shared({{dx, bytes}, {dgamma, cb}, {dbeta, cb}, {scratch, used}}, {{x, bytes}, {dy, bytes}, {gamma, cb}, {beta, cb}, {mean, sb}, {rstd, sb}}))
+    return NF_EINVAL;
   GnArgs a{};
   if (fill_gn(a, pl, N, P, C, groups, act) != NF_OK) return NF_ECUDA;
   a.x = x; a.dy = dy; a.gamma = gamma; a.beta = beta; a.out = dx; a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);

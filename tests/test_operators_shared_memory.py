@@ -1,0 +1,40 @@
+"""Every output that shares memory with an input, with scratch or with another output is refused, through the C ABI without a GPU: the refusal comes
+before any device work, so the addresses are never used."""
+import ctypes as C
+
+import pytest
+
+A = [C.c_void_p(0x100000 * (i + 1)) for i in range(14)]
+
+
+@pytest.fixture(scope="module")
+def nf():
+    from paper_2402_14139_b200 import build
+    build.build()
+    from paper_2402_14139_b200 import nf as mod
+    return mod
+
+
+def _all_refused(nf, f, args, written, read, both_ways=()):
+    """Each tensor of `written` (argument positions) laid over each other tensor's first and last bytes.  read, written: {position: bytes}."""
+    n = 0
+    for w, nw in written.items():
+        for o, no in {**read, **written}.items():
+            if o == w or args[o] is None or (w, o) in both_ways:
+                continue
+            for at in (args[o].value, args[o].value + (no - 1) // 16 * 16, args[o].value - (nw - 1) // 16 * 16):
+                bad = list(args)
+                bad[w] = C.c_void_p(at)
+                assert f(*bad) == nf.NF_EINVAL, (f.__name__, w, o, at - args[o].value)
+                n += 1
+    return n
+
+
+def test_group_norm(nf):
+    L, N, P, C_, G = nf.lib(), 2, 40, 64, 4
+    x, c, s = N * P * C_ * 2, C_ * 4, N * G * 4
+    assert _all_refused(nf, L.nf_group_norm_forward, [1, A[0], A[1], A[2], N, P, C_, G, 1e-5, 1, A[3], A[4], A[5]],
+                        {10: x, 11: s, 12: s}, {1: x, 2: c, 3: c}) == 45
+    sb = L.nf_group_norm_scratch_bytes(1, N, P, C_, G)
+    assert _all_refused(nf, L.nf_group_norm_backward, [1, A[0], A[1], A[2], A[3], A[4], A[5], N, P, C_, G, 1, A[6], sb, A[7], A[8], A[9]],
+                        {12: sb, 14: x, 15: c, 16: c}, {1: x, 2: x, 3: c, 4: c, 5: s, 6: s}) == 108
