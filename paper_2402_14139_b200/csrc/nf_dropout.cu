@@ -77,7 +77,7 @@ extern "C" int nf_dropout(int dtype, const void* x, long long n, float p, unsign
   if (!x || !y || n < 1 || (dtype != NF_F32 && dtype != NF_BF16) || !(p >= 0.f && p < 1.f)) return NF_EINVAL;
   if (((uintptr_t)x | (uintptr_t)y) & 15 || (uintptr_t)offset_dev & 7) return NF_EALIGN;
   const size_t bytes = (size_t)n * nf_esize(dtype);
-  if (x != y && nf_overlap(x, bytes, y, bytes)) return NF_EINVAL;
+  if ((x != y && nf_overlap(x, bytes, y, bytes)) || nf_overlap(y, bytes, offset_dev, 8)) return NF_EINVAL;
   const uint32_t threshold = (uint32_t)((double)p * 4294967296.0);  // p < 1 as a float is at most 1 - 2^-24
   const float scale = (float)(1.0 / (1.0 - (double)p));
   if ((size_t)n / 2048 >= 0x7fffffffull) return NF_EUNSUPPORTED;

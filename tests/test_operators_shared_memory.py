@@ -38,3 +38,11 @@ def test_group_norm(nf):
     sb = L.nf_group_norm_scratch_bytes(1, N, P, C_, G)
     assert _all_refused(nf, L.nf_group_norm_backward, [1, A[0], A[1], A[2], A[3], A[4], A[5], N, P, C_, G, 1, A[6], sb, A[7], A[8], A[9]],
                         {12: sb, 14: x, 15: c, 16: c}, {1: x, 2: x, 3: c, 4: c, 5: s, 6: s}) == 108
+
+
+def test_dropout(nf):
+    """The offset on the device may not lie in y: blocks read it while others write."""
+    L, n = nf.lib(), 1000
+    for at in (0, 8, n * 2 - 8):
+        assert L.nf_dropout(1, A[0], n, 0.5, 1, 2, C.c_void_p(A[1].value + at), A[1]) == nf.NF_EINVAL
+        assert L.nf_dropout(1, A[1], n, 0.5, 1, 2, C.c_void_p(A[1].value + at), A[1]) == nf.NF_EINVAL
