@@ -328,7 +328,7 @@ int nf_conv3x3_wgrad_static(int dtype, const void* x, const void* g, int N, int 
  * activation cache in 8 bits.  (The paper's networks are VGG and ResNet shapes: a classifier of linear layers with dropout stands
  * behind their last block, 1x1 convolutions are linear layers over pixels, and at the batch sizes of a few images that small memory
  * budgets force, group normalisation replaces batch statistics.)  All pointers device unless said otherwise, 16-byte aligned, tensors dense and
- * channels-last; outputs must not share memory with inputs or scratch except where a call says so.  Parameters, statistics and parameter gradients are float,
+ * channels-last; outputs must not share memory with one another, with inputs or with scratch except where a call says so (NF_EINVAL).  Parameters, statistics and parameter gradients are float,
  * activations and their gradients of `dtype`, linear weights of `dtype`.  Arithmetic and sums in fp32 or more, each output rounded once.
  * Results do not depend on launch order: the same call on the same data gives the same bits.  Asynchronous on the library's stream, and
  * recordable into a CUDA graph after a first eager call with the same arguments.  Concurrent calls need scratch of their own. */

@@ -299,8 +299,11 @@ extern "C" int nf_cache_gather_quantized(int format, const void* codes, const fl
   if ((cache_labels == nullptr) != (out_labels == nullptr)) return NF_EINVAL;
   if (((uintptr_t)codes | (uintptr_t)scales | (uintptr_t)out) & 15) return NF_EALIGN;
   if (((uintptr_t)idx | (uintptr_t)cache_labels | (uintptr_t)out_labels) & 3) return NF_EALIGN;
-  const size_t ob = (size_t)count * row_elems * nf_esize(dtype);
-  if (nf_overlap(out, ob, codes, (size_t)cache_rows * row_elems) || nf_overlap(out, ob, scales, (size_t)cache_rows * ((row_elems + group - 1) / group) * 4))
+  const size_t ob = (size_t)count * row_elems * nf_esize(dtype), nb = (size_t)count * 4;
+  if (nf_shared({{out, ob}, {out_labels, nb}}, {{codes, (size_t)cache_rows * row_elems},
+                                                {scales, (size_t)cache_rows * ((row_elems + group - 1) / group) * 4},
+                                                {cache_labels, (size_t)cache_rows * 4},
+                                                {idx, nb}}))
     return NF_EINVAL;
   int32_t* st = nullptr;
   if (nf_tc_op_status_ptr(&st) != NF_OK) return NF_ECUDA;

@@ -46,3 +46,22 @@ def test_dropout(nf):
     for at in (0, 8, n * 2 - 8):
         assert L.nf_dropout(1, A[0], n, 0.5, 1, 2, C.c_void_p(A[1].value + at), A[1]) == nf.NF_EINVAL
         assert L.nf_dropout(1, A[1], n, 0.5, 1, 2, C.c_void_p(A[1].value + at), A[1]) == nf.NF_EINVAL
+
+
+def test_gather_from_the_quantised_cache(nf):
+    L, rows, count, E, group = nf.lib(), 50, 40, 1000, 64
+    args = [0, A[0], A[1], A[2], rows, A[3], count, E, group, 1, A[4], A[5]]
+    read = {1: rows * E, 2: rows * 16 * 4, 3: rows * 4, 5: count * 4}
+    assert _all_refused(nf, L.nf_cache_gather_quantized, args, {10: count * E * 2, 11: count * 4}, read) == 30
+
+
+def test_linear_and_cache_write(nf):
+    """As before: these calls compared every pair already."""
+    L, M, K, N = nf.lib(), 40, 64, 48
+    x, w, y, b = M * K * 2, N * K * 2, M * N * 2, N * 4
+    sb = L.nf_linear_scratch_bytes(1, M, K, N)
+    assert _all_refused(nf, L.nf_linear_forward, [1, A[0], A[1], A[2], A[3], M, K, N, 1, A[4], sb, A[5], A[6]], {9: sb, 11: y, 12: y},
+                        {1: x, 2: w, 3: b, 4: y}) == 54
+    assert _all_refused(nf, L.nf_linear_dgrad, [1, A[0], A[1], M, K, N, A[2], sb, A[3]], {6: sb, 8: x}, {1: y, 2: w}) == 18
+    assert _all_refused(nf, L.nf_linear_wgrad, [1, A[0], A[1], M, K, N, A[2], sb, A[3], A[4]], {6: sb, 8: 2 * w, 9: b}, {1: x, 2: y}) == 36
+    assert _all_refused(nf, L.nf_cache_quantize, [0, 1, A[0], 4, 1000, 64, A[1], A[2]], {6: 4000, 7: 4 * 16 * 4}, {2: 8000}) == 12
