@@ -138,12 +138,19 @@ class QuantizedCache:
         self.codes = torch.empty(self.shape, dtype=torch.uint8, **where)
         self.scales = torch.empty((shape[0], n), dtype=torch.float32, **where)
 
+    def stage(self, torch, N, device):
+        """Two (codes, scales) buffers on the device for chunks of N rows, or (None, None) where the quantiser can write the cache in place: it lies on
+        the device and every chunk starts at a multiple of 16 bytes in both tensors."""
+        if self.is_cuda and N * self.codes[0].numel() % 16 == 0 and N * self.scales.shape[1] % 4 == 0:
+            return None, None
+        return tuple((torch.empty((N,) + self.shape[1:], dtype=torch.uint8, device=device), torch.empty((N, self.scales.shape[1]), device=device))
+                     for _ in range(2))
+
     def _dt(self, nf):
         return nf.NF_F32 if self.tdtype.itemsize == 4 else nf.NF_BF16
 
     def write(self, nf, start, x, stage):
-        """Rows start ... of the cache from the activations x on the device; stage: (codes, scales) buffers on the device where the
-        cache lies in host memory, else None."""
+        """Rows start ... of the cache from the activations x on the device; stage: one of the buffers of stage()."""
         n = x.shape[0]
         codes, scales = (self.codes[start:start + n], self.scales[start:start + n]) if stage is None else (stage[0][:n], stage[1][:n])
         nf.nf_cache_quantize(self.fmt, self._dt(nf), x, self.group, codes, scales)
@@ -305,8 +312,7 @@ def train_blockwise(nf, torch, wl, data, labels, epochs=1, lr=0.01, seed=1, log=
         in_dev = (not disk_in) and (not coded_in) and cur.is_cuda
         stage_in = None if in_dev else torch.empty((N,) + tuple(cur.shape[1:]), dtype=tdt, device=dev)
         stage_out = [torch.empty((N,) + oshape[1:], dtype=tdt, device=dev) for _ in range(2)] if (host or disk or cache_format) else None
-        stage_codes = [(torch.empty((N,) + oshape[1:], dtype=torch.uint8, device=dev), torch.empty((N, out.scales.shape[1]), device=dev))
-                       for _ in range(2)] if cache_format and host else None
+        stage_codes = out.stage(torch, N, dev) if cache_format else None
         t1 = time.perf_counter()
         pending = []      # disk: (chunk start, count, buffer) whose device -> pinned copy is in flight
         for ci, s in enumerate(range(0, K, N)):
@@ -332,9 +338,9 @@ def train_blockwise(nf, torch, wl, data, labels, epochs=1, lr=0.01, seed=1, log=
                 pin_out[b][:cnt].copy_(stage_out[b][:cnt].view(torch.int16), non_blocking=True)
                 done_out[b].record(main)
                 pending.append((s, cnt, b))
-            elif cache_format:            # forward into a device chunk, quantised into the cache (by way of the device where it is pinned)
+            elif cache_format:            # forward into a device chunk, quantised into the cache (by way of a buffer where it cannot be in place)
                 block.cache(src, stage_out[ci % 2][:cnt], count=cnt)
-                out.write(nf, s, stage_out[ci % 2][:cnt], stage_codes[ci % 2] if host else None)
+                out.write(nf, s, stage_out[ci % 2][:cnt], stage_codes[ci % 2])
             elif host:                    # forward into a device chunk, then an asynchronous copy to the pinned cache
                 so = stage_out[ci % 2]
                 block.cache(src, so[:cnt], count=cnt)
