@@ -206,13 +206,23 @@ def evaluate_exits(nf, torch, layers, N, val_cur, val_labels):
     return counts.cpu().tolist(), out
 
 
+def _check_operators(nf, what):
+    """Raises what the stand-alone operations have reported since the last look (nf_op_status), each bit under its own name."""
+    status = nf.nf_op_status()
+    if status == nf.NF_ENONFINITE:
+        raise RuntimeError(f"{what}: activations that are not finite cannot be cached in 8 bits")
+    if status:
+        names = [n for n in ("NF_ELABEL", "NF_ENONFINITE", "NF_ETIMEOUT", "NF_EINDEX") if status & getattr(nf, n)]
+        raise RuntimeError(f"{what}: stand-alone operations report {' | '.join(names)} ({status})")
+
+
 def train_blockwise(nf, torch, wl, data, labels, epochs=1, lr=0.01, seed=1, log=None, val=None, cache="hbm", spill_dir=None,
                     offload=None, cache_format=None, cache_group=64):
     """data: device (or pinned host) tensor [K, H, W, C] of the first layer's dtype; labels: device int32 [K];
     cache: "hbm" keeps each block's output for all samples on the device, "host" in pinned host memory, "disk" in a
     memory-mapped file under spill_dir (bf16 workloads);
     cache_format: None keeps the activations' type; "int8" or "e4m3" (not with "disk") stores 8-bit codes, one scale per cache_group elements, and
-    the cached output returned is a QuantizedCache;
+    the cached output returned is a QuantizedCache; what earlier stand-alone operations of the caller have left in nf_op_status() is then cleared;
     offload: None keeps nothing of a finished block but its cache; "host" stores its layers' state (Layer.export_state) in
     the block's record under "state"; a directory path writes block<i>.npz there and records the path;
     val: optional (device tensor [V, H, W, C], device int32 [V]) validation set.
@@ -221,6 +231,10 @@ def train_blockwise(nf, torch, wl, data, labels, epochs=1, lr=0.01, seed=1, log=
     K = data.shape[0]
     if cache_format is not None and cache == "disk":
         raise ValueError('cache_format needs cache="hbm" or "host"')
+    if cache_format is not None:
+        if cache_format not in nf.CACHE_FORMATS or cache_group not in (32, 64, 128):
+            raise ValueError(f"cache_format {cache_format!r}, cache_group {cache_group!r}: one of {sorted(nf.CACHE_FORMATS)}; 32, 64 or 128")
+        nf.nf_op_status()
     report = []
     cur = data
     labels_host = labels.cpu().numpy() if cache == "disk" else None
@@ -289,9 +303,11 @@ def train_blockwise(nf, torch, wl, data, labels, epochs=1, lr=0.01, seed=1, log=
             keep = keep[-3:]
         torch.cuda.synchronize()
         t_train = time.perf_counter() - t0
-        status = [L.status() for L in layers] + ([nf.nf_op_status()] if cache_format else [])
+        status = [L.status() for L in layers]
         if any(status):
             raise RuntimeError(f"block {bi}: device status {status}")
+        if cache_format:
+            _check_operators(nf, f"block {bi}")
         # fill the cache: the block's output for every sample, in chunks of the block's batch size
         last = layers[-1]
         oshape = (K, last.Ha, last.Wa, last.Cout)
@@ -348,8 +364,8 @@ def train_blockwise(nf, torch, wl, data, labels, epochs=1, lr=0.01, seed=1, log=
             else:
                 block.cache(src, out[s:s + cnt], count=cnt)
         torch.cuda.synchronize()
-        if cache_format and nf.nf_op_status():
-            raise RuntimeError(f"block {bi}: activations that are not finite cannot be cached in 8 bits")
+        if cache_format:
+            _check_operators(nf, f"block {bi}")
         for s0, c0, b0 in pending:
             out[s0:s0 + c0] = pin_out[b0][:c0].numpy()
         if disk:
