@@ -337,7 +337,8 @@ enum nf_act { NF_ACT_NONE = 0, NF_ACT_RELU = 1, NF_ACT_SILU = 2, NF_ACT_GELU = 3
 /* Group normalisation with the activation behind it.  x, y: [N][P][C], P pixels per image; the C channels form `groups` groups of
  * neighbours; gamma, beta: [C]; mean, rstd: [N][groups] (written, for the backward pass):
  *   y = act(gamma xh + beta),  xh = (x - mean) rstd,  rstd = 1 / sqrt(variance + eps), biased variance over P * C/groups values.
- * Backward: dy the gradient at y; dx the gradient at x; dgamma, dbeta: [C].  Needs nf_group_norm_scratch_bytes() of scratch (overwritten).  A ReLU is
+ * Backward: dy the gradient at y; dx the gradient at x; dgamma, dbeta: [C].  Needs nf_group_norm_scratch_bytes() of scratch (overwritten), which
+ * covers every smaller N as well.  A ReLU is
  * open in it where gamma xh + beta is above 0 with every operation rounded to fp32 by itself.
  * NF_EINVAL: sizes < 1, C not a multiple of groups, eps not above 0; NF_EUNSUPPORTED: more than 4096 channels in a group,
  * 2^24 channels, 2^30 images or pixels. */
@@ -354,7 +355,7 @@ int nf_group_norm_backward(int dtype, const void* x, const void* dy, const float
  *                    be dy's or saved's memory.  Not needed without an activation: then g = dy.
  *   nf_linear_dgrad: dx = g w [M][K].
  *   nf_linear_wgrad: dw = g^T x, float [N][K]; db = column sums of g, float [N], or NULL.
- * All but nf_act_backward need nf_linear_scratch_bytes() of scratch (overwritten).  Sums are held in fp32, in runs of at most 1024 products where the
+ * All but nf_act_backward need nf_linear_scratch_bytes() of scratch (overwritten), which covers every smaller M as well.  Sums are held in fp32, in runs of at most 1024 products where the
  * tensor cores, which cut a running sum off instead of rounding it, add them.  fp32 operands have to be finite and below 2^127 in
  * magnitude: an infinity among them may give NaN instead of an infinity; operands below 2^-102 may lose digits.  NF_EINVAL: sizes < 1; NF_EUNSUPPORTED: sizes
  * above 2^30, results of more than 2^22 - 64 columns (N forward, K of dx and dw), db of more than 2^21 - 32. */

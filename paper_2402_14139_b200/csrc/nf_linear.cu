@@ -630,16 +630,50 @@ int simple_splits(int P, int Q, int R) {
   return s < 1 ? 1 : (int)s;
 }
 
-size_t product_bytes(int dtype, const Product& d) {
-  const bool tc = on_tensor_cores(dtype, d);
-  const int s = tc ? nf_gemm_splits(d.P, d.Q, d.R, dtype == NF_F32 ? 3 : 1) : simple_splits(d.P, d.Q, d.R);
-  size_t b = s > 1 ? (size_t)s * d.P * d.Q * 4 : 0;
-  if (few_across(dtype, d)) {
-    const int n = dtype == NF_F32 ? across_splits<float>(d.P, d.Q, d.R) : across_splits<bf16>(d.P, d.Q, d.R);
-    return (size_t)n * d.P * d.Q * 4;
+// Scratch that covers a product of M rows and every one of fewer, so that what was allocated for the largest batch serves a ragged last one: fewer rows
+// mean more splits, and other kernels.  Copies of operands grow with M.  Partial sums:
+//  - where P is M (forward, input gradient) splits * tiles <= `places` bounds splits * P by places * side / (tiles along q), and splits and P each have a bound of
+//    their own; across_splits likewise, over the P that across() takes;
+//  - where R is M (weight gradient) splits grow with it; the simple kernel's as far as it is used.
+size_t split_bytes(int P, int Q, long most, int side, long places) {
+  const long tq = (Q + side - 1) / side;
+  if (most < 2 || places / tq < 2) return 0;
+  const double rows = (double)most * P, cap = (double)places * side / tq;
+  return (size_t)(rows < cap ? rows : cap) * Q * 4;
+}
+template <typename T>
+size_t across_bytes(const Product& d) {
+  constexpr int cols = 512 / (int)sizeof(T);
+  if (d.Q % (16 / (int)sizeof(T))) return 0;
+  const double columns = (double)nf_align_up(d.Q, cols) * d.R, fit = (sizeof(T) == 4 ? 67108864.0 : 16777216.0) / columns;
+  double P = fit < (double)(1 << 17) ? fit : (double)(1 << 17);
+  if (P < kAcrossMost<T>) P = kAcrossMost<T>;
+  if (P > d.P) P = d.P;
+  const long blocks = (d.Q + cols - 1) / cols;
+  double rows = 0;
+  if (592 / blocks >= 2 && d.R >= 128) {
+    rows = (double)(d.R / 64) * P;
+    const double cap = 592.0 * kAcrossRows<T> / blocks;
+    if (rows > cap) rows = cap;
   }
-  if (tc) b += copy_bytes(dtype, d.a_rows(), d.a_len()) + copy_bytes(dtype, d.b_rows(), d.b_len());
-  return b;
+  const double forced = (d.R - 1) / 4096 + 1;
+  if (forced > 1 && rows < forced * P) rows = forced * P;
+  return (size_t)rows * d.Q * 4;
+}
+size_t product_bytes(int dtype, const Product& d) {
+  const bool f32 = dtype == NF_F32;
+  size_t sums = 0;
+  auto most = [&](size_t b) { sums = b > sums ? b : sums; };
+  if (d.a_along_r) {
+    most(split_bytes(d.P, d.Q, nf_gemm_splits(1, 1, d.R, f32 ? 3 : 1), 128, 148));
+    if (f32) most(split_bytes(d.P, d.Q, d.R / 128, 64, 296));
+    if (!d.b_along_r) most(f32 ? across_bytes<float>(d) : across_bytes<bf16>(d));
+  } else {
+    auto whole = [&](int s) { most(s > 1 ? (size_t)s * d.P * d.Q * 4 : 0); };
+    whole(nf_gemm_splits(d.P, d.Q, d.R, f32 ? 3 : 1));
+    if (f32) whole(simple_splits(d.P, d.Q, d.R));
+  }
+  return sums + (on_tensor_cores(dtype, d) ? copy_bytes(dtype, d.a_rows(), d.a_len()) + copy_bytes(dtype, d.b_rows(), d.b_len()) : 0);
 }
 
 template <typename T>

@@ -1239,6 +1239,23 @@ GnPlan plan_gn(int dtype, int N, int P, int C, int groups, bool bwd) {
 // Counts of images and pixels run on in steps beyond the last one, channels are doubled: all in 32 bits
 bool gn_size_ok(int N, int P, int C, int groups) { return C / groups <= kMaxCs && N <= 1 << 30 && P <= 1 << 30 && C <= 1 << 24; }
 
+// Rows of partial sums that the backward pass needs at most, for N images or fewer: what was allocated for the largest batch then serves a ragged last one
+// (fewer images get more blocks each).  A plan has at most 16 blocks to an image, and more rows than 16 only for as many as there are teams (eight to a block)
+// for each slice; the generic form's slices may be one.
+size_t gn_rows(int dtype, int N, int C, int groups) {
+  const int full = 16 / (int)nf_esize(dtype);
+  int least, most;
+  size_t rows = kMaxBlocks;
+  if (slice_lanes(C, C / groups, full, &least, &most)) {
+    const size_t held = (size_t)296 * (kNT / 32) * (most * full) / C;  // `most` lanes make the fewest slices
+    const int wide = most < 8 ? most : 8 > least ? 8 : least;
+    if (wide * full / (C / groups) <= 32) rows = held;
+  }
+  if (rows < kMaxCluster) rows = kMaxCluster;
+  const size_t few = (size_t)N * kMaxCluster;
+  return (few < rows ? few : rows) + kNT / 32 - 1;  // rounded up to whole blocks of teams
+}
+
 bool gn_args_ok(int dtype, int N, int P, int C, int groups) {
   return (dtype == NF_F32 || dtype == NF_BF16) && N >= 1 && P >= 1 && C >= 1 && groups >= 1 && C % groups == 0;
 }
@@ -1360,7 +1377,7 @@ extern "C" int nf_group_norm_forward(int dtype, const void* x, const float* gamm
 
 extern "C" size_t nf_group_norm_scratch_bytes(int dtype, int N, int P, int C, int groups) {
   if (!gn_args_ok(dtype, N, P, C, groups) || !gn_size_ok(N, P, C, groups)) return 0;
-  return (size_t)plan_gn(dtype, N, P, C, groups, true).rows * 2 * C * sizeof(float);
+  return gn_rows(dtype, N, C, groups) * 2 * C * sizeof(float);
 }
 
 extern "C" int nf_group_norm_backward(int dtype, const void* x, const void* dy, const float* gamma, const float* beta, const float* mean,
@@ -1375,8 +1392,9 @@ extern "C" int nf_group_norm_backward(int dtype, const void* x, const void* dy, 
   if (!gn_size_ok(N, P, C, groups)) return NF_EUNSUPPORTED;
   const size_t bytes = (size_t)N * P * C * nf_esize(dtype);
   GnPlan pl = plan_gn(dtype, N, P, C, groups, true);
-  if (scratch_bytes < (size_t)pl.rows * 2 * C * sizeof(float)) return NF_ENOWS;
-  const size_t used = (size_t)pl.rows * 2 * C * sizeof(float), cb = (size_t)C * 4, sb = (size_t)N * groups * 4;
+  const size_t used = gn_rows(dtype, N, C, groups) * 2 * C * sizeof(float);
+  if (scratch_bytes < used) return NF_ENOWS;
+  const size_t cb = (size_t)C * 4, sb = (size_t)N * groups * 4;
   if (nf_shared({{dx, bytes}, {dgamma, cb}, {dbeta, cb}, {scratch, used}}, {{x, bytes}, {dy, bytes}, {gamma, cb}, {beta, cb}, {mean, sb}, {rstd, sb}}))
     return NF_EINVAL;
   GnArgs a{};
