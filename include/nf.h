@@ -329,7 +329,8 @@ int nf_conv3x3_wgrad_static(int dtype, const void* x, const void* g, int N, int 
  * behind their last block, 1x1 convolutions are linear layers over pixels, and at the batch sizes of a few images that small memory
  * budgets force, group normalisation replaces batch statistics.)  All pointers device unless said otherwise, 16-byte aligned, tensors dense and
  * channels-last; outputs must not share memory with one another, with inputs or with scratch except where a call says so (NF_EINVAL).  Parameters, statistics and parameter gradients are float,
- * activations and their gradients of `dtype`, linear weights of `dtype`.  Arithmetic and sums in fp32 or more, each output rounded once.
+ * activations and their gradients of `dtype`, linear weights of `dtype`.  Arithmetic and sums in fp32 or more, each output rounded once; with bf16 storage the
+ * exponential in SiLU and GELU, and with it the parameter gradients, is good to a relative 2^-22 (1 + |z|) or so, 2^-23 (1 + z^2) in GELU.
  * Results do not depend on launch order: the same call on the same data gives the same bits.  Asynchronous on the library's stream, and
  * recordable into a CUDA graph after a first eager call with the same arguments.  Concurrent calls need scratch of their own. */
 enum nf_act { NF_ACT_NONE = 0, NF_ACT_RELU = 1, NF_ACT_SILU = 2, NF_ACT_GELU = 3 };  /* GELU: z times the normal distribution function of z */

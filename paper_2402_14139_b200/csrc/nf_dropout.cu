@@ -35,8 +35,8 @@ __device__ __forceinline__ void drop8(float (&v)[8], const uint4& a, const uint4
   }
 }
 
-// Eight elements (two blocks of the generator) per thread.  Its integer arithmetic bounds bf16: about 140 instructions per thread, the most
-// of them on the integer pipe; 70 M elements 64 us (4.4 TB/s), fp32 35 M 48 us (5.8 TB/s).  Blocks that stride over the tensor with the
+// Eight elements (two blocks of the generator) per thread.  The generator bounds bf16: about 140 instructions per thread in ten rounds that depend on one
+// another, the most of them on the integer pipe, which is 59% busy, issue slots 61%; 70 M elements 64 us (4.4 TB/s), fp32 35 M 48 us (5.8 TB/s).  Blocks that stride over the tensor with the
 // next pieces on their way took longer (72 us with one piece, 87 with two: fewer threads to hide the rounds' latency), and so did four pieces a
 // thread (95 us).  WIDE: block numbers beyond 32 bits.
 template <typename T, bool WIDE>

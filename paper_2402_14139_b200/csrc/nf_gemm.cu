@@ -13,8 +13,8 @@
 // l h, h l, m m, h m, m h, h h; what is left out is below 2^-24 of |x| |w|.  The three parts of a step of 64 lie in three stages side by side,
 // so that each is brought in once for all its products.
 //
-// What bounds it: the tensor pipe where sums are long (gradients of 8602 x 8192 -> 4096: the two products 725 us, 1.59 PFLOP/s, the pipe 93% and 88%
-// busy), memory where they are short (200704 x 256 x 256 with residual: 65 us, 4.7 TB/s), the ends of the pipeline and the join of partial
+// What bounds it: the tensor pipe where sums are long (gradients of 8602 x 8192 -> 4096: the two products 728 us, 1.59 PFLOP/s, the pipe 91% and 86%
+// busy), the epilogue's latency where they are short (200704 x 256 x 256 with residual: 65 us, 4.7 TB/s, DRAM 51% and issue slots 26% busy), the ends of the pipeline and the join of partial
 // sums where the result has few tiles (128 x 4096 x 4096: 17 us, its weights alone 5).  For those, clusters that join a tile's sums through
 // distributed shared memory took 16.4 us there but 14 instead of 12 at 1000 x 1000 x 1000, and pairs of blocks on 256 x 128 tiles 10.6 there and
 // 35.7 instead of 26.5 at 318 x 2408 x 840 fp32: neither is here.

@@ -11,9 +11,11 @@
 //  - any other shape: a cluster of blocks reads its slice twice, the second time from L2.
 // Parameter gradients gather in registers or shared memory over all images of a team or block, then in one row of partials each.
 //
-// What bounds it: HBM with ReLU or none (8602 maps of 4x4x512 backward 78 us, 5.5 TB/s; 256 images of 112x112x64 forward 162 us, 5.1 TB/s), the
-// special-function and FMA pipes with SiLU or GELU, whose derivative is taken in both passes (128 images of 32x32x128 backward 42 us, 2.4 TB/s),
-// and for images of several MB the second reading: 64 of 224x224x64 forward 205 us, of which L2 gives back a quarter of what is read twice.
+// What bounds it: HBM with ReLU or none (8602 maps of 4x4x512 backward 78 us, 5.5 TB/s, and 88 with the launch that joins dgamma and dbeta; 256 images of
+// 112x112x64 forward 160 us, 5.1 TB/s, in groups of two channels 196), latency with SiLU or GELU, whose derivative is taken in both passes: the pieces of the
+// ring go one at a time through a wait and the sigmoid's chain (128 images of 32x32x128 backward 42 us, 2.4 TB/s, with the special-function pipe 41%
+// and the issue slots 43% busy), and for images of several MB the second reading: 64 of 224x224x64 forward 210 us, of which L2 gives back a quarter
+// of what is read twice.
 //
 // Sums of the forward pass: a thread takes its values in runs of a few dozen, subtracts the mean of what it has seen before (of its first few pixels
 // to begin with), and joins a run's mean and squared deviations to those of the runs before it; lanes, warps and blocks are joined in the same way.  So neither
