@@ -18,9 +18,10 @@
 // of what is read twice.
 //
 // Sums of the forward pass: a thread takes its values in runs of a few dozen, subtracts the mean of what it has seen before (of its first few pixels
-// to begin with), and joins a run's mean and squared deviations to those of the runs before it; lanes, warps and blocks are joined in the same way.  So neither
-// a mean far from zero nor a value that is not like the others costs digits: in any run the squares added are at most about as large as the
-// deviations that come out.  The backward pass adds in fp32 what a thread sees, then in fp32 or fp64 over threads and blocks; its ReLU mask is decided on
+// to begin with), and joins a run's mean and squared deviations to those of the runs before it; lanes, warps and blocks are joined in the same way.  A mean is
+// held as two numbers, what was subtracted and the distance from it, until it leaves the block: rounded to one it would be off by 2^-24 of itself, and the
+// squares of distances between such means by as much of their product.  So neither a mean far from zero nor a value that is not like the others costs
+// digits: in any run the squares added are at most about as large as the deviations that come out.  The backward pass adds in fp32 what a thread sees, then in fp32 or fp64 over threads and blocks; its ReLU mask is decided on
 // xh gamma + beta with every operation rounded by itself.
 #include <cooperative_groups.h>
 
@@ -223,9 +224,10 @@ __global__ void __launch_bounds__(kNT, V == 8 ? 2 : 4) group_norm_kernel(const G
   nf_pdl_begin();
   constexpr int NP = (V + 1) / 2, U = V < 8 || BWD ? 4 : 8;  // loads in flight per thread and tensor
   extern __shared__ __align__(16) float sm[];
-  float* red = sm;                        // [2V + 1][kNT] tree reduction
-  float* tot = red + (2 * V + 1) * kNT;   // [2][2][Cs] this block's channel sums (forward: means, squared deviations), two images in turn
-  float* gsm = tot + 4 * a.Cs;            // [2][groups of the slice]: mean and rstd (forward), m1 and m2 (backward)
+  constexpr int kSums = BWD ? 2 : 3;
+  float* red = sm;                        // [kSums V + 1][kNT] tree reduction
+  float* tot = red + (kSums * V + 1) * kNT;  // [2][kSums][Cs] this block's channel sums (forward: mean as distance and from where, squared deviations), two images in turn
+  float* gsm = tot + 2 * kSums * a.Cs;            // [2][groups of the slice]: mean and rstd (forward), m1 and m2 (backward)
   float* acc = gsm + 2 * (a.Cs / a.cpg);  // backward: [2][Cs] sums over the images of this block
   cg::cluster_group cluster = cg::this_cluster();
   const int rank = blockIdx.x % a.CS, cid = blockIdx.x / a.CS, slice = cid % a.slices;
@@ -248,42 +250,47 @@ __global__ void __launch_bounds__(kNT, V == 8 ? 2 : 4) group_norm_kernel(const G
   for (int n = cid / a.slices; n < a.N; n += a.stride, turn ^= 1) {
     const size_t base = (size_t)n * a.P * a.C + c0;
     const size_t gbase = (size_t)n * a.G + slice * gps;
-    float* mine = tot + turn * 2 * a.Cs;
+    float* mine = tot + turn * kSums * a.Cs;
     auto saved = [&](int g) { return make_float2(a.mean[gbase + g], a.rstd[gbase + g]); };
     for (int cv0 = 0; cv0 < a.vpr; cv0 += cols) {
       const int cv = cv0 + tc;
       f32x2 s[NP], q[NP];
-      [[maybe_unused]] f32x2 mu[NP], m2[NP], nk[NP];  // forward: mean and squared deviations of the pixels seen, minus what is subtracted
+      // Forward: minus what is subtracted, the distance from that of the mean of the pixels seen, and their squared deviations
+      [[maybe_unused]] f32x2 nk[NP], mu[NP], m2[NP];
       [[maybe_unused]] float seen = 0.f;
 #pragma unroll
-      for (int i = 0; i < NP; ++i) s[i] = q[i] = mu[i] = m2[i] = 0;
+      for (int i = 0; i < NP; ++i) s[i] = q[i] = nk[i] = mu[i] = m2[i] = 0;
       if (on && cv < a.vpr) {
         const size_t col = base + (size_t)cv * V;
         if constexpr (BWD) {
           if (!one_col) ch.affine(a, c0 + cv * V);
           ch.stats(cv * V, a.cpg, saved);
         }
-        auto subtract = [&](int i) { nk[i] = nf_pack2(-finite_or_0(low(mu[i])), -finite_or_0(high(mu[i]))); };
-        [[maybe_unused]] auto begin = [&](const Raw<T, V>* v, auto pixels) {  // the mean of the first pixels
+        auto finite2 = [](f32x2 v) { return nf_pack2(finite_or_0(low(v)), finite_or_0(high(v))); };
+        auto minus = [](f32x2 v) { return nf_mul2(v, both(-1.f)); };
+        [[maybe_unused]] auto begin = [&](const Raw<T, V>* v, auto pixels) {  // the mean of the first pixels is subtracted from the first run
           constexpr int n = decltype(pixels)::value;
 #pragma unroll
           for (int i = 0; i < NP; ++i) {
+            f32x2 m = 0;
 #pragma unroll
-            for (int u = 0; u < n; ++u) mu[i] = nf_fma2(v[u].pair(i), both(1.f / n), mu[i]);
-            subtract(i);
-            mu[i] = nf_mul2(nk[i], both(-1.f));
+            for (int u = 0; u < n; ++u) m = nf_fma2(v[u].pair(i), both(1.f / n), m);
+            nk[i] = minus(finite2(m));
           }
         };
-        [[maybe_unused]] auto join = [&](int pixels) {  // deviations from mu: new mean = mu + s / n, squared deviations from it + q - s^2 / n
+        // `pixels` have been added as distances from -nk, `seen` lie mu from there: S = s + seen mu of n, the mean lies S / n from there, and the squared
+        // deviations grow by q + seen mu^2 - S^2 / n.  Then the mean, rounded, is what is subtracted.
+        [[maybe_unused]] auto join = [&](int pixels) {
           const float n = seen + (float)pixels;
           const f32x2 w = both(1.f / n);
 #pragma unroll
           for (int i = 0; i < NP; ++i) {
-            const f32x2 d = nf_mul2(s[i], w);
-            m2[i] = nf_add2(m2[i], nf_fma2(nf_mul2(s[i], both(-1.f)), d, q[i]));
-            mu[i] = nf_add2(mu[i], d);
+            const f32x2 old = nf_mul2(both(seen), mu[i]), sum = nf_add2(s[i], old), d = nf_mul2(sum, w);
+            m2[i] = nf_add2(m2[i], nf_fma2(minus(sum), d, nf_fma2(old, mu[i], q[i])));
+            const f32x2 next = minus(finite2(nf_add2(d, minus(nk[i]))));
+            mu[i] = nf_add2(d, nf_add2(next, minus(nk[i])));
+            nk[i] = next;
             s[i] = q[i] = 0;
-            subtract(i);
           }
           seen = n;
         };
@@ -351,7 +358,11 @@ __global__ void __launch_bounds__(kNT, V == 8 ? 2 : 4) group_norm_kernel(const G
         red[i * kNT + threadIdx.x] = i % 2 ? high(first) : low(first);
         red[(V + i) * kNT + threadIdx.x] = i % 2 ? high(second) : low(second);
       }
-      if constexpr (!BWD) red[2 * V * kNT + threadIdx.x] = seen;
+      if constexpr (!BWD) {
+        red[3 * V * kNT + threadIdx.x] = seen;
+#pragma unroll
+        for (int i = 0; i < V; ++i) red[(2 * V + i) * kNT + threadIdx.x] = i % 2 ? high(nk[i / 2]) : low(nk[i / 2]);
+      }
       for (int left = R; left > 1;) {
         const int half = (left + 1) / 2;
         __syncthreads();
@@ -361,17 +372,18 @@ __global__ void __launch_bounds__(kNT, V == 8 ? 2 : 4) group_norm_kernel(const G
           if constexpr (BWD) {
 #pragma unroll
             for (int e = 0; e < 2 * V; ++e) mine_at[e * kNT] += other[e * kNT];
-          } else {  // (count, mean, squared deviations) of both; rows further on never have more pixels
-            const float na = mine_at[2 * V * kNT], nb = other[2 * V * kNT];
+          } else {  // (count, what was subtracted, distance of the mean, squared deviations) of both; rows further on never have more pixels
+            const float na = mine_at[3 * V * kNT], nb = other[3 * V * kNT];
             if (nb > 0.f) {
               const float w = __fdividef(nb, na + nb);  // two units in the last place are enough for a weight
 #pragma unroll
               for (int e = 0; e < V; ++e) {
-                const float ma = mine_at[e * kNT], mb = other[e * kNT], base_m = finite_or_0(ma), d = mb - ma;
+                const float ma = mine_at[e * kNT], base_m = finite_or_0(ma);
+                const float mb = (mine_at[(2 * V + e) * kNT] - other[(2 * V + e) * kNT]) + other[e * kNT], d = mb - ma;
                 mine_at[e * kNT] = base_m + fmaf(mb - base_m, w, (ma - base_m) * (1.f - w));
                 mine_at[(V + e) * kNT] += other[(V + e) * kNT] + d * d * (na * w);
               }
-              mine_at[2 * V * kNT] = na + nb;
+              mine_at[3 * V * kNT] = na + nb;
             }
           }
         }
@@ -379,7 +391,7 @@ __global__ void __launch_bounds__(kNT, V == 8 ? 2 : 4) group_norm_kernel(const G
       }
       __syncthreads();
       const int width = (a.vpr - cv0 < cols ? a.vpr - cv0 : cols) * V;  // channels of this chunk
-      for (int i = threadIdx.x; i < 2 * width; i += kNT) {
+      for (int i = threadIdx.x; i < kSums * width; i += kNT) {
         const int w = i / width, c = i - w * width;
         mine[w * a.Cs + cv0 * V + c] = red[(w * V + c % V) * kNT + c / V];
       }
@@ -393,9 +405,9 @@ __global__ void __launch_bounds__(kNT, V == 8 ? 2 : 4) group_norm_kernel(const G
       const int lane = threadIdx.x % L, per = kNT / L;
       for (int g0 = 0; g0 < gps; g0 += per) {
         const int g = g0 + threadIdx.x / L;
-        double A = 0, B = 0, from = 0;  // forward: moments about the first channel's mean in the first block
+        double A = 0, B = 0, from = 0;  // forward: moments about what the first block subtracted from the group's first channel
         if (g < gps) {
-          if constexpr (!BWD) from = finite_or_0(cluster.map_shared_rank(mine, 0)[g * a.cpg]);
+          if constexpr (!BWD) from = -cluster.map_shared_rank(mine, 0)[2 * a.Cs + g * a.cpg];
           for (int i = lane; i < a.cpg; i += L) {
             const int c = g * a.cpg + i;
             double S = 0, Q = 0;
@@ -406,7 +418,7 @@ __global__ void __launch_bounds__(kNT, V == 8 ? 2 : 4) group_norm_kernel(const G
                 S += o[c];
                 Q += o[a.Cs + c];
               } else {  // CS is a power of two
-                const double n = (double)(int)(((long long)a.P * (r + 1) >> cs_log) - ((long long)a.P * r >> cs_log)), d = o[c] - from;
+                const double n = (double)(int)(((long long)a.P * (r + 1) >> cs_log) - ((long long)a.P * r >> cs_log)), d = o[c] - ((double)o[2 * a.Cs + c] + from);
                 S += n * d;
                 Q += o[a.Cs + c] + n * d * d;
               }
@@ -519,8 +531,6 @@ __global__ void __launch_bounds__(kNT, V == 8 ? 2 : 4) group_norm_kernel(const G
 // barrier guards the data.  Sums of a group (forward: means and squared deviations): shuffles; teams of several warps join one pair per warp and group
 // through shared memory; blocks of a cluster send theirs to each other (st.async into slots of the receiver, counted by its barrier).  FINE: groups of fewer channels than a piece;
 // MORE: the slice is larger than what is held.
-constexpr int kSlotGroups = 64;
-
 __device__ __forceinline__ void copy16(uint32_t to, const void* from) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
@@ -540,7 +550,7 @@ template <typename T, int V, int ACT, bool BWD, bool FINE, bool MORE>
 __global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a) {
   constexpr int NT = kNT, NP = V / 2, S = FINE ? V : 1, kTensors = BWD ? 2 : 1, kRing = held_ring(BWD);
   extern __shared__ __align__(16) uint8_t held_raw[];
-  __shared__ float part[NT / 32][2][kSlotGroups];        // per warp: totals of the slots (groups, or FINE channels)
+  __shared__ float part[NT / 32][BWD ? 2 : 3][32];      // per warp: totals of the groups
   __shared__ float2 gsm[NT / 32 * 32];                  // per team: mean and rstd, or m1 and m2
   __shared__ float2 peers[2][kMaxCluster][32];          // the blocks' totals, two items in turn
   __shared__ uint64_t xbar[2];
@@ -714,29 +724,32 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a)
         for (int i = 1; i < V; ++i) to[0] += v[i];
       }
     };
-    // Forward: mean and squared deviations of what this thread has seen of its group, or FINE of each channel, and minus what is subtracted from
-    // the next values
-    [[maybe_unused]] float mu = 0.f, sq = 0.f;
-    [[maybe_unused]] f32x2 mu2[NP], sq2[NP], nk[NS];
-    auto subtract = [&] {
-#pragma unroll
-      for (int i = 0; i < NS; ++i)
-        nk[i] = FINE ? nf_pack2(-finite_or_0(low(mu2[i])), -finite_or_0(high(mu2[i]))) : both(-finite_or_0(mu));
-    };
-    // Deviations from that have been added: new mean = mu + s / n, squared deviations from it + q - s^2 / n.  w = 1 / n
+    // Forward: minus what is subtracted (of the group, or FINE of each channel), the distance from that of the mean of what this thread has seen, and its
+    // squared deviations; seen: how much that is
+    [[maybe_unused]] f32x2 nk[NS] = {}, mu2[NP], sq2[NP];
+    [[maybe_unused]] float mu = 0.f, sq = 0.f, seen = 0.f;
+    auto finite2 = [](f32x2 v) { return nf_pack2(finite_or_0(low(v)), finite_or_0(high(v))); };
+    // Values have been added as distances from -nk: S = s + seen mu of n = 1 / w, the mean lies S / n from there, the squared deviations grow by
+    // q + seen mu^2 - S^2 / n.  Then the mean, rounded, is what is subtracted.
     auto join_run = [&](float w) {
       if constexpr (FINE) {
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-          sq2[i] = nf_add2(sq2[i], nf_fma2(nf_mul2(s[i], both(-w)), s[i], q[i]));
-          mu2[i] = nf_fma2(s[i], both(w), mu2[i]);
+          const f32x2 old = nf_mul2(both(seen), mu2[i]), sum = nf_add2(s[i], old), d = nf_mul2(sum, both(w));
+          sq2[i] = nf_add2(sq2[i], nf_fma2(nf_mul2(sum, both(-1.f)), d, nf_fma2(old, mu2[i], q[i])));
+          const f32x2 minus = both(-1.f), next = nf_mul2(finite2(nf_fma2(nk[i], minus, d)), minus);
+          mu2[i] = nf_add2(d, nf_fma2(nk[i], minus, next));
+          nk[i] = next;
         }
       } else {
         float f0[S], f1[S];
         slots(s, f0);
         slots(q, f1);
-        sq += fmaf(f0[0] * -w, f0[0], f1[0]);
-        mu = fmaf(f0[0], w, mu);
+        const float old = seen * mu, sum = f0[0] + old, d = sum * w;
+        sq += fmaf(-sum, d, fmaf(old, mu, f1[0]));
+        const float before = -low(nk[0]), next = finite_or_0(before + d);
+        mu = d - (next - before);
+        nk[0] = both(-next);
       }
 #pragma unroll
       for (int i = 0; i < NP; ++i) s[i] = q[i] = 0;
@@ -776,7 +789,7 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a)
       if constexpr (!BWD) {  // what is subtracted to begin with: the mean of the first four pieces
         f32x2 sum[NP];
 #pragma unroll
-        for (int i = 0; i < NP; ++i) sum[i] = sq2[i] = 0;
+        for (int i = 0; i < NP; ++i) sum[i] = mu2[i] = sq2[i] = 0;
         auto more = [&](const Raw<T, V>& v) {
 #pragma unroll
           for (int i = 0; i < NP; ++i) sum[i] = nf_fma2(v.pair(i), both(pivot_w), sum[i]);
@@ -785,12 +798,11 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a)
           if constexpr (!FINE) {
             float m[S];
             slots(sum, m);
-            mu = finite_or_0(m[0]);
+            nk[0] = both(-finite_or_0(m[0]));
           } else {
 #pragma unroll
-            for (int i = 0; i < NP; ++i) mu2[i] = nf_pack2(finite_or_0(low(sum[i])), finite_or_0(high(sum[i])));
+            for (int i = 0; i < NP; ++i) nk[i] = nf_mul2(finite2(sum[i]), both(-1.f));
           }
-          subtract();
         };
         if (kw >= 4) {
           Raw<T, V> v[4];
@@ -820,11 +832,9 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a)
     }
     if constexpr (!BWD) {
       if constexpr (MORE) {
-        float seen = 0.f;
         ring_use(add, forth, kw, [&] {
+          join_run(1.f / (seen + kRun * unit));
           seen += kRun * unit;
-          join_run(1.f / seen);
-          subtract();
         });
       }
       join_run(own_w);
@@ -853,17 +863,35 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a)
             if (BWD || !FINE || !(i & (a.cpg - 1))) w[i] += __shfl_xor_sync(0xffffffffu, w[i], o);
         }
     };
-    float f[2][S];  // backward: sums; forward: mean and squared deviations
+    float f[2][S];  // backward: sums; forward: distance of the mean from `origin`, squared deviations
+    [[maybe_unused]] float origin[S];
     if constexpr (BWD) {
       slots(s, f[0]);
       slots(q, f[1]);
       over_lanes(f);
-    } else {
+    } else {  // the origin: what the first lane of the group subtracted; no lane has more pixels
+#pragma unroll
+      for (int i = 0; i < S; ++i)
+        if (!FINE || !(i & (a.cpg - 1))) origin[i] = -__shfl_sync(0xffffffffu, i % 2 ? high(nk[i / 2]) : low(nk[i / 2]), from_lane);
+      auto spread = [&](float (&v)[S]) {  // from a group's first channel
+        if constexpr (FINE) {
+#pragma unroll
+          for (int i = 1; i < S; ++i) {
+            if (i % 2 && a.cpg >= 2) v[i] = v[i - 1];
+            if (i % 4 == 2 && a.cpg >= 4) v[i] = v[i - 2];
+          }
+        }
+      };
+      spread(origin);
       if constexpr (FINE) {  // channels of a group: as many pixels of each
         f32x2 v[NP];
         const f32x2 w = both(1.f / a.cpg), px = both((float)own_px);
 #pragma unroll
-        for (int i = 0; i < NP; ++i) v[i] = nf_mul2(mu2[i], w);
+        for (int i = 0; i < NP; ++i) {  // from the origin on
+          const f32x2 from = nf_add2(nk[i], nf_pack2(origin[2 * i], origin[S > 1 ? 2 * i + 1 : 0]));
+          mu2[i] = nf_fma2(from, both(-1.f), mu2[i]);
+          v[i] = nf_mul2(mu2[i], w);
+        }
         slots(v, f[0]);
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
@@ -872,19 +900,16 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a)
         }
         slots(v, f[1]);
       } else {
-        f[0][0] = mu;
+        f[0][0] = mu - (low(nk[0]) + origin[0]);
         f[1][0] = sq;
       }
-      float m[S], from[S];
+      float m[S];
 #pragma unroll
-      for (int i = 0; i < S; ++i) {
-        from[i] = finite_or_0(__shfl_sync(0xffffffffu, f[0][i], from_lane));  // no lane of the group has more pixels
-        m[i] = own_n * (f[0][i] - from[i]);
-      }
+      for (int i = 0; i < S; ++i) m[i] = own_px ? own_n * f[0][i] : 0.f;
       over_lanes(m);
 #pragma unroll
       for (int i = 0; i < S; ++i) {
-        m[i] = fmaf(m[i], warp_w, from[i]);
+        m[i] *= warp_w;
         const float d = f[0][i] - m[i];
         f[0][i] = m[i];
         f[1][i] = own_px ? fmaf(own_n * d, d, f[1][i]) : 0.f;
@@ -892,16 +917,8 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a)
       over_lanes(f[1]);
 #pragma unroll
       for (int i = 0; i < S; ++i) f[1][i] = f[1][i] < 0.f ? 0.f : f[1][i];  // a NaN stays one
-      if constexpr (FINE) {
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-#pragma unroll
-          for (int i = 1; i < S; ++i) {
-            if (i % 2 && a.cpg >= 2) f[w][i] = f[w][i - 1];
-            if (i % 4 == 2 && a.cpg >= 4) f[w][i] = f[w][i - 2];
-          }
-        }
-      }
+      spread(f[0]);
+      spread(f[1]);
     }
     const float M = (float)a.P * a.cpg;
     float2 mine[S];
@@ -911,7 +928,7 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a)
         if constexpr (BWD) {
           mine[i] = make_float2(-f[0][i] / M, -f[1][i] / M);
         } else {
-          mine[i] = make_float2(f[0][i], 1.f / sqrtf(f[1][i] / M + a.eps));
+          mine[i] = make_float2(origin[i] + f[0][i], 1.f / sqrtf(f[1][i] / M + a.eps));
         }
       }
       if (!BWD && tr == 0 && tc % lo == 0) {
@@ -931,6 +948,7 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a)
             const int g = (tc * V + i) / a.cpg;
             part[threadIdx.x / 32][0][g] = f[0][i];
             part[threadIdx.x / 32][1][g] = f[1][i];
+            if constexpr (!BWD) part[threadIdx.x / 32][2][g] = origin[i];
           }
       }
       ptx::named_barrier(1 + team, TS);
@@ -946,16 +964,19 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a)
           A = __shfl_sync(0xffffffffu, v, 0);
           B = __shfl_sync(0xffffffffu, v, 16);
         } else {
-          const float wn = lane < warps ? warp_values(lane) : 0.f, wm = wn > 0.f ? part[team * warps + lane][0][g] : 0.f;
-          const float from = finite_or_0(__shfl_sync(0xffffffffu, wm, 0));  // no warp has more pixels than the first
-          A = wn > 0.f ? wn * (wm - from) : 0.f;
+          const float wn = lane < warps ? warp_values(lane) : 0.f, wo = wn > 0.f ? part[team * warps + lane][2][g] : 0.f;
+          const float from = __shfl_sync(0xffffffffu, wo, 0);  // no warp has more pixels than the first
+          const float wm = wn > 0.f ? (wo - from) + part[team * warps + lane][0][g] : 0.f;
+          A = wn * wm;
 #pragma unroll
           for (int o = 1; o < NT / 32; o *= 2) A += __shfl_xor_sync(0xffffffffu, A, o);
-          A = from + (np ? __shfl_sync(0xffffffffu, A, 0) / ((float)np * a.cpg) : 0.f);
+          A = __shfl_sync(0xffffffffu, A, 0);
+          if (np) A /= (float)np * a.cpg;
           B = wn > 0.f ? fmaf(wn * (wm - A), wm - A, part[team * warps + lane][1][g]) : 0.f;
 #pragma unroll
           for (int o = 1; o < NT / 32; o *= 2) B += __shfl_xor_sync(0xffffffffu, B, o);
           B = __shfl_sync(0xffffffffu, B, 0);
+          A += from;
         }
         if (a.CS > 1) {
           if (t == 0 && g == 0) ptx::mbar_expect_tx(&xbar[turn], a.CS * gps * 8);  // once: the barrier counts one arrival
@@ -1234,7 +1255,7 @@ GnPlan plan_gn(int dtype, int N, int P, int C, int groups, bool bwd) {
   pl.stride = (int)most;
   pl.rows = (int)most * pl.CS;
   const int Cs = C / pl.slices;
-  pl.smem = sizeof(float) * ((size_t)(2 * pl.V + 1) * kNT + 4 * Cs + 2 * (Cs / cpg) + (bwd ? 2 * Cs : 0));
+  pl.smem = sizeof(float) * ((size_t)((bwd ? 2 : 3) * pl.V + 1) * kNT + 6 * Cs + 2 * (Cs / cpg));
   return pl;
 }
 

@@ -7,8 +7,10 @@ of the runs.  p is the mean of its first m pixels (n / m <= 10) or of all it has
     adds M2 + D^2 n N / (n + N) to the deviations, D its mean's distance from p, and q = M2 + n D^2 is at most (1 + n / N) times that, n / N < 2.  So
     all that is ever added is at most 11 times the deviations that come out.
   - q is rounded n + V + 2 <= 50 times and s^2 / n, at most q, twice that relative to q: independent roundings of at most u of a running sum, together about
-    u sqrt(50 / 3) (1 + 2) q <= 12 u q <= 135 u M2.  Joins of lanes, warps and blocks are a few roundings of positive numbers each: 10 u.  rstd has half
-    the relative error of the variance and a rounding or two of its own: 75 u.  The tests allow 128 u = 2^-17.
+    u sqrt(50 / 3) (1 + 2) q <= 12 u q <= 135 u M2.  Joins of lanes, warps and blocks are a few roundings of positive numbers each: 10 u.
+  - A mean leaves a thread as two numbers.  It is rounded to one behind 32 values or more of a block, by u |mean|, and moves the squared deviations by
+    2 u |mean| sigma / sqrt(32) at most in each block's share, independently: u |mean| / (4 sigma) of the variance in sixteen blocks, 62 u below.
+  - rstd has half the relative error of the variance and a rounding or two of its own: 75 u, 106 u where the mean is 1000 sigma.  Allowed: 128 u = 2^-17.
   - A mean is off by u sqrt(50 / 3) times the root of q / n in a run, 3 sigma at most: 12 u sigma, and by u |mean| where it is rounded: at every join,
     independently, at most 64 of them: 8 u |mean|.  Allowed: 32 u sigma + 16 u |mean|.
   - xh = (x - mean) rstd follows: E = u (128 |xh| + 32 + 16 |mean| rstd), and a few roundings of xh, z and the activation.
@@ -142,6 +144,18 @@ def test_a_first_value_far_from_the_others(env, si, dtype):
     x[:, 0] = 0
     x[:, -1] = 0
     if P > 3:
+        _Case(env, x, G, "none", dtype).check_forward(statistics_only=True)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("si", range(len(SHAPES)))
+def test_a_mean_far_from_zero(env, si, dtype):
+    """Values around 1000 with a deviation of 1: a mean of a few pixels that was rounded to fp32 would be off by 1000 u, and the squares of distances
+    between such means by twice that."""
+    _, torch = env
+    N, P, C, G = SHAPES[si]
+    for P in {P, 3, 6, 40}:
+        x = _randn(torch, (min(N, 400), P, C), 50 + si) + 1000
         _Case(env, x, G, "none", dtype).check_forward(statistics_only=True)
 
 
