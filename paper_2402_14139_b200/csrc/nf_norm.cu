@@ -19,7 +19,7 @@
 //
 // Sums of the forward pass: a thread takes its values in runs of a few dozen, subtracts the mean of what it has seen before (of its first few pixels
 // to begin with), and joins a run's mean and squared deviations to those of the runs before it; lanes, warps and blocks are joined in the same way.  A mean is
-// held as two numbers, what was subtracted and the distance from it, until it leaves the block: rounded to one it would be off by 2^-24 of itself, and the
+// held as two numbers, what was subtracted and the distance from it, until it is stored: rounded to one it would be off by 2^-24 of itself, and the
 // squares of distances between such means by as much of their product.  So neither a mean far from zero nor a value that is not like the others costs
 // digits: in any run the squares added are at most about as large as the deviations that come out.  The backward pass adds in fp32 what a thread sees, then in fp32 or fp64 over threads and blocks; its ReLU mask is decided on
 // xh gamma + beta with every operation rounded by itself.
@@ -553,6 +553,7 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a)
   __shared__ float part[NT / 32][BWD ? 2 : 3][32];      // per warp: totals of the groups
   __shared__ float2 gsm[NT / 32 * 32];                  // per team: mean and rstd, or m1 and m2
   __shared__ float2 peers[2][kMaxCluster][32];          // the blocks' totals, two items in turn
+  __shared__ float peers_rest[BWD ? 1 : 2][kMaxCluster][32];  // forward: of their means, what rounding left
   __shared__ uint64_t xbar[2];
   __shared__ int abort_word;
   const int TS = a.TS, team = threadIdx.x / TS, t = threadIdx.x % TS, lane = threadIdx.x & 31, warps = TS / 32;
@@ -956,6 +957,7 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a)
       // a warp per group: its lanes join the warps' sums (A in the lower half, B in the upper), then the other blocks'
       for (int g = t / 32; g < gps; g += warps) {
         float A, B;
+        [[maybe_unused]] float rest_of_mean = 0.f;
         if constexpr (BWD) {
           const int w = lane & 15;
           float v = w < warps ? part[team * warps + w][lane >> 4][g] : 0.f;
@@ -976,11 +978,18 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a)
 #pragma unroll
           for (int o = 1; o < NT / 32; o *= 2) B += __shfl_xor_sync(0xffffffffu, B, o);
           B = __shfl_sync(0xffffffffu, B, 0);
-          A += from;
+          const float sum = from + finite_or_0(A);
+          rest_of_mean = A - (sum - from);
+          A = sum;
         }
         if (a.CS > 1) {
-          if (t == 0 && g == 0) ptx::mbar_expect_tx(&xbar[turn], a.CS * gps * 8);  // once: the barrier counts one arrival
-          if (lane < a.CS) ptx::st_async_f2(&peers[turn][rank][g], A, B, &xbar[turn], lane);
+          if (t == 0 && g == 0) ptx::mbar_expect_tx(&xbar[turn], a.CS * gps * (BWD ? 8 : 12));  // once: the barrier counts one arrival
+          if (lane < a.CS) {
+            ptx::st_async_f2(&peers[turn][rank][g], A, B, &xbar[turn], lane);
+            if constexpr (!BWD) ptx::st_async_f1(&peers_rest[turn][rank][g], rest_of_mean, &xbar[turn], lane);
+          }
+        } else if (!BWD) {
+          A += rest_of_mean;
         }
         if (lane == 0) own[g] = make_float2(A, B);
       }
@@ -991,8 +1000,9 @@ __global__ void __launch_bounds__(kNT, 2) group_norm_held_kernel(const GnArgs a)
           if (g == t / 32) ptx::mbar_wait(&xbar[turn], (xph >> turn) & 1, &abort_word);  // sets the abort word itself when it gives up
           const float2 from = lane < a.CS ? peers[turn][lane][g] : make_float2(0.f, 0.f);
           const float cr = lane < a.CS ? (float)max(0, min(a.P - lane * a.rpc, a.rpc)) : 0.f;
-          const float base = finite_or_0(__shfl_sync(0xffffffffu, from.x, 0));  // block 0 has pixels: means are joined by their distances from its mean
-          const float d = BWD ? from.x : cr > 0.f ? from.x - base : 0.f;
+          const float base = __shfl_sync(0xffffffffu, from.x, 0);  // forward, block 0's mean, rounded, which is finite: means are joined by their distances from it
+          float d = from.x;
+          if constexpr (!BWD) d = cr > 0.f ? (from.x - base) + peers_rest[turn][lane & (kMaxCluster - 1)][g] : 0.f;
           float m = BWD ? d : cr * d, M2 = from.y;
 #pragma unroll
           for (int o = 1; o < kMaxCluster; o *= 2) m += __shfl_xor_sync(0xffffffffu, m, o);

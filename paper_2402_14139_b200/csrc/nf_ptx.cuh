@@ -189,6 +189,14 @@ __device__ __forceinline__ void st_async_f2(const void* dst, float x, float y, u
       "f"(x), "f"(y), "r"(smem_u32(bar)), "r"(rank)
       : "memory");
 }
+// One float likewise (4 bytes)
+__device__ __forceinline__ void st_async_f1(const void* dst, float x, uint64_t* bar, uint32_t rank) {
+  asm volatile(
+      "{\n.reg .b32 rd, rb;\nmapa.shared::cluster.u32 rd, %0, %3;\nmapa.shared::cluster.u32 rb, %2, %3;\n"
+      "st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.f32 [rd], %1, [rb];\n}" ::"r"(smem_u32(dst)),
+      "f"(x), "r"(smem_u32(bar)), "r"(rank)
+      : "memory");
+}
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));

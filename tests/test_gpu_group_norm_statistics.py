@@ -8,9 +8,8 @@ of the runs.  p is the mean of its first m pixels (n / m <= 10) or of all it has
     all that is ever added is at most 11 times the deviations that come out.
   - q is rounded n + V + 2 <= 50 times and s^2 / n, at most q, twice that relative to q: independent roundings of at most u of a running sum, together about
     u sqrt(50 / 3) (1 + 2) q <= 12 u q <= 135 u M2.  Joins of lanes, warps and blocks are a few roundings of positive numbers each: 10 u.
-  - A mean leaves a thread as two numbers.  It is rounded to one behind 32 values or more of a block, by u |mean|, and moves the squared deviations by
-    2 u |mean| sigma / sqrt(32) at most in each block's share, independently: u |mean| / (4 sigma) of the variance in sixteen blocks, 62 u below.
-  - rstd has half the relative error of the variance and a rounding or two of its own: 75 u, 106 u where the mean is 1000 sigma.  Allowed: 128 u = 2^-17.
+  - A mean is held as two numbers until it is stored, so distances between means are rounded relative to themselves: they count among the joins.
+  - rstd has half the relative error of the variance and a rounding or two of its own: 75 u.  Allowed: 128 u = 2^-17.
   - A mean is off by u sqrt(50 / 3) times the root of q / n in a run, 3 sigma at most: 12 u sigma, and by u |mean| where it is rounded: at every join,
     independently, at most 64 of them: 8 u |mean|.  Allowed: 32 u sigma + 16 u |mean|.
   - xh = (x - mean) rstd follows: E = u (128 |xh| + 32 + 16 |mean| rstd), and a few roundings of xh, z and the activation.
@@ -157,6 +156,13 @@ def test_a_mean_far_from_zero(env, si, dtype):
     for P in {P, 3, 6, 40}:
         x = _randn(torch, (min(N, 400), P, C), 50 + si) + 1000
         _Case(env, x, G, "none", dtype).check_forward(statistics_only=True)
+
+
+def test_a_mean_far_from_zero_in_small_blocks(env):
+    """Clusters whose blocks have 36 values of a group, means of up to 4000 sigma."""
+    _, torch = env
+    x = _randn(torch, (10, 283, 64), 51) + 1000 * _randn(torch, (10, 1, 64), 52)
+    _Case(env, x, 64, "none", 0).check_forward(statistics_only=True)
 
 
 @pytest.mark.parametrize("size", [100.0, 1e4])
