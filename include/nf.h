@@ -328,7 +328,8 @@ int nf_conv3x3_wgrad_static(int dtype, const void* x, const void* g, int N, int 
  * activation cache in 8 bits.  (The paper's networks are VGG and ResNet shapes: a classifier of linear layers with dropout stands
  * behind their last block, 1x1 convolutions are linear layers over pixels, and at the batch sizes of a few images that small memory
  * budgets force, group normalisation replaces batch statistics.)  All pointers device unless said otherwise, 16-byte aligned, tensors dense and
- * channels-last; outputs must not share memory with one another, with inputs or with scratch except where a call says so (NF_EINVAL).  Parameters, statistics and parameter gradients are float,
+ * channels-last; outputs must not share memory with one another, with inputs or with scratch except where a call says so (NF_EINVAL).
+ * Parameters, statistics and parameter gradients are float,
  * activations and their gradients of `dtype`, linear weights of `dtype`.  Arithmetic and sums in fp32 or more, each output rounded once; with bf16 storage the
  * exponential in SiLU and GELU, and with it the parameter gradients, is good to a relative 2^-22 (1 + |z|) or so, 2^-23 (1 + z^2) in GELU.
  * Results do not depend on launch order: the same call on the same data gives the same bits.  Asynchronous on the library's stream, and
@@ -356,8 +357,8 @@ int nf_group_norm_backward(int dtype, const void* x, const void* dy, const float
  *                    be dy's or saved's memory.  Not needed without an activation: then g = dy.
  *   nf_linear_dgrad: dx = g w [M][K].
  *   nf_linear_wgrad: dw = g^T x, float [N][K]; db = column sums of g, float [N], or NULL.
- * All but nf_act_backward need nf_linear_scratch_bytes() of scratch (overwritten), which covers every smaller M as well.  Sums are held in fp32, in runs of at most 1024 products where the
- * tensor cores, which cut a running sum off instead of rounding it, add them.  fp32 operands have to be finite and below 2^127 in
+ * All but nf_act_backward need nf_linear_scratch_bytes() of scratch (overwritten), which covers every smaller M as well.  Sums
+ * are held in fp32, in runs of at most 1024 products where the tensor cores, which cut a running sum off instead of rounding it, add them.  fp32 operands have to be finite and below 2^127 in
  * magnitude: an infinity among them may give NaN instead of an infinity; operands below 2^-102 may lose digits.  NF_EINVAL: sizes < 1; NF_EUNSUPPORTED: sizes
  * above 2^30, results of more than 2^22 - 64 columns (N forward, K of dx and dw), db of more than 2^21 - 32. */
 int nf_linear_forward(int dtype, const void* x, const void* w, const float* bias, const void* residual, int M, int K, int N, int act, void* scratch,

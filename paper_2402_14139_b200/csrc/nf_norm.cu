@@ -12,17 +12,17 @@
 // Parameter gradients gather in registers or shared memory over all images of a team or block, then in one row of partials each.
 //
 // What bounds it: HBM with ReLU or none (8602 maps of 4x4x512 backward 78 us, 5.5 TB/s, and 88 with the launch that joins dgamma and dbeta; 256 images of
-// 112x112x64 forward 160 us, 5.1 TB/s, in groups of two channels 196), latency with SiLU or GELU, whose derivative is taken in both passes: the pieces of the
+// 112x112x64 forward 160 us, 5.1 TB/s, in groups of two channels 201), latency with SiLU or GELU, whose derivative is taken in both passes: the pieces of the
 // ring go one at a time through a wait and the sigmoid's chain (128 images of 32x32x128 backward 42 us, 2.4 TB/s, with the special-function pipe 41%
-// and the issue slots 43% busy), and for images of several MB the second reading: 64 of 224x224x64 forward 210 us, of which L2 gives back a quarter
+// and the issue slots 43% busy), and for images of several MB the second reading: 64 of 224x224x64 forward 212 us, of which L2 gives back a quarter
 // of what is read twice.
 //
 // Sums of the forward pass: a thread takes its values in runs of a few dozen, subtracts the mean of what it has seen before (of its first few pixels
 // to begin with), and joins a run's mean and squared deviations to those of the runs before it; lanes, warps and blocks are joined in the same way.  A mean is
 // held as two numbers, what was subtracted and the distance from it, until it is stored: rounded to one it would be off by 2^-24 of itself, and the
 // squares of distances between such means by as much of their product.  So neither a mean far from zero nor a value that is not like the others costs
-// digits: in any run the squares added are at most about as large as the deviations that come out.  The backward pass adds in fp32 what a thread sees, then in fp32 or fp64 over threads and blocks; its ReLU mask is decided on
-// xh gamma + beta with every operation rounded by itself.
+// digits: in any run the squares added are at most about as large as the deviations that come out.  The backward pass adds in fp32
+// what a thread sees, then in fp32 or fp64 over threads and blocks; its ReLU mask is decided on xh gamma + beta with every operation rounded by itself.
 #include <cooperative_groups.h>
 
 #include <cuda.h>
@@ -226,7 +226,8 @@ __global__ void __launch_bounds__(kNT, V == 8 ? 2 : 4) group_norm_kernel(const G
   extern __shared__ __align__(16) float sm[];
   constexpr int kSums = BWD ? 2 : 3;
   float* red = sm;                        // [kSums V + 1][kNT] tree reduction
-  float* tot = red + (kSums * V + 1) * kNT;  // [2][kSums][Cs] this block's channel sums (forward: mean as distance and from where, squared deviations), two images in turn
+  // [2][kSums][Cs] this block's channel sums, two images in turn; forward: the mean's distance from what was subtracted, squared deviations, minus that
+  float* tot = red + (kSums * V + 1) * kNT;
   float* gsm = tot + 2 * kSums * a.Cs;            // [2][groups of the slice]: mean and rstd (forward), m1 and m2 (backward)
   float* acc = gsm + 2 * (a.Cs / a.cpg);  // backward: [2][Cs] sums over the images of this block
   cg::cluster_group cluster = cg::this_cluster();
@@ -529,8 +530,8 @@ __global__ void __launch_bounds__(kNT, V == 8 ? 2 : 4) group_norm_kernel(const G
 // of a pixel, a power of two up to 32, whole groups; a thread takes pieces t, t + TS, ..., so its channels stay the same, and it alone
 // copies them into shared memory (cp.async), reads them in both passes and refills their places with the image `buffers` turns on: no
 // barrier guards the data.  Sums of a group (forward: means and squared deviations): shuffles; teams of several warps join one pair per warp and group
-// through shared memory; blocks of a cluster send theirs to each other (st.async into slots of the receiver, counted by its barrier).  FINE: groups of fewer channels than a piece;
-// MORE: the slice is larger than what is held.
+// through shared memory; blocks of a cluster send theirs to each other (st.async into slots of the receiver, counted by its barrier).  FINE: groups
+// of fewer channels than a piece; MORE: the slice is larger than what is held.
 __device__ __forceinline__ void copy16(uint32_t to, const void* from) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
